@@ -305,6 +305,53 @@ kmip_status_t kmip_fwd_noalloc(const void* Q, const void* K, const void* V, int6
                                int32_t d, int32_t k, float scale, float* out, int32_t* topk_idx,
                                float* lse, void* stream);
 
+/*
+ * Full softmax attention over packed sequences (the attention that k-MIP
+ * approximates: every key of the query's sequence is kept), with grouped
+ * heads, an optional causal mask and keys of an earlier call:
+ *   out_i = sum_j p_ij v_j,  p_ij = exp(scale q_i.k_j - lse_i),
+ *   lse_i = log sum_j exp(scale q_i.k_j).
+ *
+ *  - Q [Nq, H, d], K [Nk, Hk, d], V [Nk, Hk, dv] of 16-bit type `dtype`; d and
+ *    dv each in {16, 32, 64, 128}; H a multiple of Hk: query head h reads key
+ *    head h / (H / Hk).  out [Nq, H, dv] of the same type; lse float32 [Nq, H].
+ *    Products are summed, and the softmax is held, in float32; the weights
+ *    are rounded to the inputs' type for the product with V.
+ *  - strides: HOST int64 [6], values between the tokens and between the heads
+ *    of Q, K and V (the last dimension has stride 1), each a multiple of 8 and
+ *    those between tokens below 2^23, or NULL: contiguous.  Views of one fused
+ *    projection are read in place.  Pointers are 16-byte aligned.  Outputs are contiguous.
+ *  - q_offsets: HOST int32 [num_seqs + 1], sequence g's queries are rows
+ *    q_offsets[g] .. q_offsets[g + 1] - 1 of Q; NULL: one sequence of all Nq.
+ *    k_offsets: the same for its slot in K and V; NULL: as q_offsets (NULL with
+ *    NULL q_offsets: all Nk).  k_lengths: HOST int32 [num_seqs], the keys in use
+ *    at the start of each slot (a cache with room behind them); NULL: the whole
+ *    slot.  Keys behind them are not read.  Sequences may be empty on either side.
+ *    All three are read before the call returns and travel in the kernels'
+ *    arguments: nothing is uploaded, so the call can be captured into a HIP
+ *    graph, which keeps the values of the capture.
+ *  - causal != 0: the queries are the last of the sequence's positions: query t
+ *    of a sequence with m queries and n keys sees keys 0 .. t + n - m.
+ *  - A query that sees no key has out = 0 and lse = -inf.
+ *  - NaN and Inf in the inputs give undefined (but memory-safe) results in the
+ *    rows of their own sequence.
+ *  - Nq * H and Nk below 2^31 - 4096; products of sizes and strides may pass 32 bits.
+ *  - workspace: kmip_full_fwd_workspace_size() bytes (often 0: then NULL is
+ *    taken), 256-byte aligned; the size depends on the offsets and lengths.
+ *  - Results do not depend on the other sequences' values and are the same from
+ *    call to call (no atomics).
+ */
+typedef enum { KMIP_BF16 = 0, KMIP_FP16 = 1, KMIP_FP32 = 2 } kmip_dtype_t;
+
+size_t kmip_full_fwd_workspace_size(const int32_t* q_offsets, const int32_t* k_offsets, const int32_t* k_lengths,
+                                    int32_t num_seqs, int64_t Nq, int64_t Nk, int32_t H, int32_t Hk, int32_t d,
+                                    int32_t dv);
+kmip_status_t kmip_full_fwd(const void* Q, const void* K, const void* V, int32_t dtype, const int64_t* strides,
+                            const int32_t* q_offsets, const int32_t* k_offsets, const int32_t* k_lengths,
+                            int32_t num_seqs, int64_t Nq, int64_t Nk, int32_t H, int32_t Hk, int32_t d, int32_t dv,
+                            float scale, int32_t causal, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                            void* stream);
+
 /* Static description of a status code. */
 const char* kmip_status_string(kmip_status_t status);
 

@@ -27,8 +27,11 @@ EXPORTS = (
     "kmip_topk_workspace_size", "kmip_topk", "kmip_topk_with_events", "kmip_attend", "kmip_fwd_workspace_size",
     "kmip_fwd", "kmip_attend_ex", "kmip_fwd_ex", "kmip_fwd_ex_with_events", "kmip_bwd_workspace_size", "kmip_bwd",
     "kmip_bwd_ex_workspace_size", "kmip_bwd_ex", "kmip_fwd_noalloc", "kmip_topk_prefilter_workspace_size",
-    "kmip_topk_prefilter", "kmip_status_string", "kmip_last_error",
+    "kmip_topk_prefilter", "kmip_full_fwd_workspace_size", "kmip_full_fwd", "kmip_status_string", "kmip_last_error",
 )
+
+# kmip_dtype_t
+BF16, FP16, FP32 = 0, 1, 2
 
 # bytes of the fixed per-device array kmip_fwd_noalloc works in
 NOALLOC_SCRATCH_BYTES = 256 * 1024 * 1024
@@ -76,9 +79,13 @@ def load(path: str = LIB_PATH):
     lib.kmip_topk_prefilter_workspace_size.argtypes = [i64, i32, i32, i32]
     lib.kmip_topk_prefilter_workspace_size.restype = sz
     lib.kmip_topk_prefilter.argtypes = [P, P, i64, i32, i32, i32, P, P, P, sz, P]
+    offsets = [P, P, P, i32, i64, i64, i32, i32, i32, i32]
+    lib.kmip_full_fwd_workspace_size.argtypes = offsets
+    lib.kmip_full_fwd_workspace_size.restype = sz
+    lib.kmip_full_fwd.argtypes = [P, P, P, i32, P, *offsets, f32, i32, P, P, P, sz, P]
     for f in ("kmip_topk", "kmip_topk_with_events", "kmip_attend", "kmip_fwd", "kmip_bwd",
               "kmip_fwd_noalloc", "kmip_attend_ex", "kmip_fwd_ex", "kmip_fwd_ex_with_events", "kmip_bwd_ex",
-              "kmip_topk_prefilter"):
+              "kmip_topk_prefilter", "kmip_full_fwd"):
         getattr(lib, f).restype = ctypes.c_int
     lib.kmip_status_string.argtypes = [ctypes.c_int]
     lib.kmip_status_string.restype = ctypes.c_char_p

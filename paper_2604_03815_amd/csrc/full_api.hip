@@ -1,0 +1,253 @@
+// Host side of full softmax attention (include/kmip.h): argument checks, the
+// cut into jobs, workspace layout and launches.
+#include <algorithm>
+#include <cstring>
+#include <new>
+
+#include "full_plan.h"
+#include "kmip.h"
+
+namespace {
+
+using kmip::FullCall;
+using kmip::FullLaunch;
+using kmip::FullPlan;
+using kmip::record_error;
+
+constexpr size_t kAlign = 256;
+size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
+
+kmip_status_t ok() { return record_error(KMIP_OK, "%s", ""); }
+
+kmip_status_t hip_fail(hipError_t e, const char* what) {
+    return record_error(KMIP_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
+}
+
+struct Seq {
+    int32_t q_lo, q_len, k_lo, k_len;
+};
+
+// Where the sequences lie; NULL offsets: see include/kmip.h.
+struct Sequences {
+    const int32_t *q, *k, *len;
+    int32_t count;
+    int64_t Nq, Nk;
+
+    Seq at(int32_t g) const {
+        if (q == nullptr) return Seq{0, (int32_t)Nq, 0, len != nullptr ? len[0] : (int32_t)Nk};
+        const int32_t* ko = k != nullptr ? k : q;
+        return Seq{q[g], q[g + 1] - q[g], ko[g], len != nullptr ? len[g] : ko[g + 1] - ko[g]};
+    }
+};
+
+kmip_status_t check_offsets(const int32_t* off, int32_t G, int64_t N, const char* name) {
+    if (off[0] != 0) return record_error(KMIP_ERR_INVALID_ARG, "%s[0]=%d must be 0", name, off[0]);
+    for (int32_t g = 0; g < G; ++g)
+        if (off[g + 1] < off[g]) return record_error(KMIP_ERR_INVALID_ARG, "%s decrease at %d", name, g);
+    if (off[G] != N) return record_error(KMIP_ERR_INVALID_ARG, "%s[G]=%d != %lld", name, off[G], (long long)N);
+    return KMIP_OK;
+}
+
+bool width_ok(int32_t d) { return d == 16 || d == 32 || d == 64 || d == 128; }
+
+kmip_status_t check_call(const int32_t* q_offsets, const int32_t* k_offsets, const int32_t* k_lengths, int32_t G,
+                         int64_t Nq, int64_t Nk, int32_t H, int32_t Hk, int32_t d, int32_t dv, Sequences* s) {
+    constexpr int64_t kMost = (int64_t(1) << 31) - 4096;
+    if (Nq < 0 || Nk < 0 || Nk >= kMost) return record_error(KMIP_ERR_INVALID_ARG, "Nq=%lld, Nk=%lld out of range", (long long)Nq, (long long)Nk);
+    if (H < 1 || Hk < 1 || H % Hk != 0)
+        return record_error(KMIP_ERR_INVALID_ARG, "H=%d must be a multiple of the %d key heads", H, Hk);
+    if (!width_ok(d) || !width_ok(dv))
+        return record_error(KMIP_ERR_UNSUPPORTED, "d=%d, d_V=%d not in {16, 32, 64, 128}", d, dv);
+    if (Nq >= kMost || Nq * (int64_t)H >= kMost) return record_error(KMIP_ERR_INVALID_ARG, "Nq*H >= 2^31 - 4096");
+    *s = Sequences{q_offsets, k_offsets, k_lengths, q_offsets != nullptr ? G : 1, Nq, Nk};
+    if (q_offsets == nullptr) {
+        if (k_offsets != nullptr) return record_error(KMIP_ERR_INVALID_ARG, "k_offsets without q_offsets");
+    } else {
+        if (G < 1) return record_error(KMIP_ERR_INVALID_ARG, "num_seqs=%d must be >= 1 with offsets", G);
+        kmip_status_t e = check_offsets(q_offsets, G, Nq, "q_offsets");
+        if (e == KMIP_OK) e = check_offsets(k_offsets != nullptr ? k_offsets : q_offsets, G, Nk, "k_offsets");
+        if (e != KMIP_OK) return e;
+    }
+    if (k_lengths != nullptr)
+        for (int32_t g = 0; g < s->count; ++g) {
+            const int64_t slot = q_offsets == nullptr ? Nk : k_offsets != nullptr ? k_offsets[g + 1] - k_offsets[g] : q_offsets[g + 1] - q_offsets[g];
+            if (k_lengths[g] < 0 || k_lengths[g] > slot)
+                return record_error(KMIP_ERR_INVALID_ARG, "k_lengths[%d]=%d outside [0, %lld]", g, k_lengths[g], (long long)slot);
+        }
+    return KMIP_OK;
+}
+
+bool finite_bits(float x) {   // (the sources are built without NaN tests)
+    uint32_t b;
+    std::memcpy(&b, &x, sizeof(b));
+    return (b & 0x7F800000u) != 0x7F800000u;
+}
+
+// Cuts the list of sequences with jobs_of(seq) jobs each into launches, the
+// costliest sequences first (ties in their order), so that the last jobs are
+// short ones.
+template <typename Jobs>
+kmip_status_t cut(std::vector<Seq>& seqs, const Jobs& jobs_of, FullPlan* p) {
+    auto cost = [](const Seq& s) { return (int64_t)std::max(s.q_len, 1) * std::max(s.k_len, 1); };
+    std::stable_sort(seqs.begin(), seqs.end(), [&](const Seq& x, const Seq& y) { return cost(x) > cost(y); });
+    p->jobs = 0;
+    for (size_t first = 0; first < seqs.size(); first += kmip::kFullSeqs) {
+        FullLaunch l{};
+        const size_t n = std::min(seqs.size() - first, (size_t)kmip::kFullSeqs);
+        int64_t jobs = 0;
+        for (size_t i = 0; i < n; ++i) {
+            const Seq& s = seqs[first + i];
+            l.seqs.q_lo[i] = s.q_lo, l.seqs.q_len[i] = s.q_len, l.seqs.k_lo[i] = s.k_lo, l.seqs.k_len[i] = s.k_len;
+            l.seqs.job0[i] = (int32_t)jobs;
+            jobs += jobs_of(s);
+            if (p->jobs + jobs >= (int64_t(1) << 31) - 1) return record_error(KMIP_ERR_INVALID_ARG, "too many rows and key runs for one call");
+        }
+        l.seqs.count = (int32_t)n;
+        l.jobs = (int32_t)jobs;
+        l.first_job = (int32_t)p->jobs;
+        p->jobs += jobs;
+        p->launches.push_back(l);
+    }
+    return KMIP_OK;
+}
+
+// The forward's jobs.
+kmip_status_t plan_fwd(const Sequences& sq, int32_t H, int32_t Hk, FullPlan* p) {
+    const int64_t rep = H / Hk;
+    std::vector<Seq> seqs;
+    int64_t rows = 0, keys = 0; // keys: over all row tiles of 32
+    for (int32_t g = 0; g < sq.count; ++g) {
+        const Seq s = sq.at(g);
+        if (s.q_len == 0) continue;
+        seqs.push_back(s);
+        const int64_t t = (s.q_len * rep + 31) / 32 * Hk;
+        rows += s.q_len * rep * Hk;
+        keys += t * s.k_len;
+    }
+    // Tiles of 128 rows once they fill the chip's 256 CUs
+    p->rows = rows >= 256 * 128 ? 128 : 32;
+    p->split = 0;
+    if (p->rows == 32) {
+        // runs of keys such that there are about 1024 jobs of like length
+        const int64_t run = std::max<int64_t>((keys / 1024 + 127) / 128 * 128, 256);
+        for (const Seq& s : seqs)
+            if (s.k_len > run) p->split = (int32_t)run;
+    }
+    const int32_t R = p->rows, split = p->split;
+    auto runs = [=](const Seq& s) { return split > 0 && s.k_len > split ? (s.k_len + (int64_t)split - 1) / split : 1; };
+    kmip_status_t e = cut(seqs, [&](const Seq& s) { return (s.q_len * rep + R - 1) / R * Hk * runs(s); }, p);
+    if (e != KMIP_OK) return e;
+    if (split > 0)
+        for (FullLaunch& l : p->launches)
+            for (int32_t i = 0; i < l.seqs.count; ++i)
+                if (l.seqs.k_len[i] > split)
+                    l.split_rows = std::max<int32_t>(l.split_rows, (int32_t)std::min<int64_t>(32, l.seqs.q_len[i] * rep));
+    return KMIP_OK;
+}
+
+// Workspace of the forward: the runs' sums, then their maxima and sums of weights.
+struct FwdLayout {
+    size_t ml, total;
+};
+FwdLayout fwd_layout(const FullPlan& p, int32_t dv) {
+    if (p.split == 0) return FwdLayout{0, 0};
+    const size_t rows = (size_t)p.jobs * p.rows;
+    const size_t ml = align_up(rows * dv * sizeof(float));
+    return FwdLayout{ml, ml + align_up(rows * 2 * sizeof(float))};
+}
+
+// A stride in values between rows of a 16-bit tensor that the kernels read 16
+// bytes at a time.
+kmip_status_t check_strides(const char* name, const void* p, int64_t row, int64_t head) {
+    if ((reinterpret_cast<uintptr_t>(p) & 15u) != 0) return record_error(KMIP_ERR_INVALID_ARG, "%s must be 16-byte aligned", name);
+    if (row < 0 || head < 0 || row % 8 != 0 || head % 8 != 0)
+        return record_error(KMIP_ERR_INVALID_ARG, "%s: strides %lld, %lld must be multiples of 8 values", name, (long long)row, (long long)head);
+    if (row >= (int64_t(1) << 23)) return record_error(KMIP_ERR_UNSUPPORTED, "%s: %lld values between rows", name, (long long)row);
+    return KMIP_OK;
+}
+
+kmip_status_t fill_call(const void* Q, const void* K, const void* V, int32_t dtype, const int64_t* strides, int64_t Nq,
+                        int64_t Nk, int32_t H, int32_t Hk, int32_t d, int32_t dv, float scale, int32_t causal, FullCall* f) {
+    if (dtype != KMIP_BF16 && dtype != KMIP_FP16) return record_error(KMIP_ERR_UNSUPPORTED, "dtype %d", dtype);
+    if (!finite_bits(scale) || !(scale > 0.0f)) return record_error(KMIP_ERR_INVALID_ARG, "scale must be finite and > 0");
+    *f = FullCall{};
+    f->q = Q, f->k = K, f->v = V;
+    f->Nq = Nq, f->Nk = Nk, f->H = H, f->Hk = Hk, f->d = d, f->dv = dv, f->causal = causal != 0;
+    f->fp16 = dtype == KMIP_FP16;
+    f->scale = scale;
+    const int64_t packed[6] = {(int64_t)H * d, d, (int64_t)Hk * d, d, (int64_t)Hk * dv, dv};
+    const int64_t* s = strides != nullptr ? strides : packed;
+    f->q_row = s[0], f->q_head = s[1], f->k_row = s[2], f->k_head = s[3], f->v_row = s[4], f->v_head = s[5];
+    f->do_row = strides != nullptr ? 0 : (int64_t)H * dv, f->do_head = strides != nullptr ? 0 : dv;
+    kmip_status_t e = KMIP_OK;
+    if (Nq > 0) e = check_strides("Q", Q, f->q_row, f->q_head);
+    if (e == KMIP_OK && Nk > 0) e = check_strides("K", K, f->k_row, f->k_head);
+    if (e == KMIP_OK && Nk > 0) e = check_strides("V", V, f->v_row, f->v_head);
+    return e;
+}
+
+kmip_status_t check_workspace(const void* ws, size_t bytes, size_t need) {
+    if (need == 0) return KMIP_OK;
+    if (ws == nullptr || bytes < need) return record_error(KMIP_ERR_WORKSPACE, "workspace of %zu bytes < %zu required", bytes, need);
+    if ((reinterpret_cast<uintptr_t>(ws) & (kAlign - 1)) != 0) return record_error(KMIP_ERR_WORKSPACE, "workspace must be 256-byte aligned");
+    return KMIP_OK;
+}
+
+// No exception crosses the ABI (the lists of jobs are the only allocations).
+template <typename F>
+kmip_status_t guarded(const F& f) {
+    try {
+        return f();
+    } catch (const std::bad_alloc&) {
+        return record_error(KMIP_ERR_INVALID_ARG, "out of host memory for the list of sequences");
+    }
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t kmip_full_fwd_workspace_size(const int32_t* q_offsets, const int32_t* k_offsets, const int32_t* k_lengths,
+                                    int32_t num_seqs, int64_t Nq, int64_t Nk, int32_t H, int32_t Hk, int32_t d, int32_t dv) {
+    size_t bytes = 0;
+    guarded([&]() {
+        Sequences sq;
+        FullPlan p;
+        kmip_status_t e = check_call(q_offsets, k_offsets, k_lengths, num_seqs, Nq, Nk, H, Hk, d, dv, &sq);
+        if (e == KMIP_OK) e = plan_fwd(sq, H, Hk, &p);
+        if (e == KMIP_OK) bytes = fwd_layout(p, dv).total;
+        return e;
+    });
+    return bytes;
+}
+
+kmip_status_t kmip_full_fwd(const void* Q, const void* K, const void* V, int32_t dtype, const int64_t* strides,
+                            const int32_t* q_offsets, const int32_t* k_offsets, const int32_t* k_lengths,
+                            int32_t num_seqs, int64_t Nq, int64_t Nk, int32_t H, int32_t Hk, int32_t d, int32_t dv,
+                            float scale, int32_t causal, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                            void* stream) {
+    return guarded([&]() {
+        Sequences sq;
+        FullCall f;
+        FullPlan p;
+        kmip_status_t e = check_call(q_offsets, k_offsets, k_lengths, num_seqs, Nq, Nk, H, Hk, d, dv, &sq);
+        if (e == KMIP_OK && Nq > 0 && (!Q || !out || !lse || (Nk > 0 && (!K || !V))))
+            e = record_error(KMIP_ERR_INVALID_ARG, "null buffer passed to kmip_full_fwd");
+        if (e == KMIP_OK) e = fill_call(Q, K, V, dtype, strides, Nq, Nk, H, Hk, d, dv, scale, causal, &f);
+        if (e == KMIP_OK && Nq > 0 && (reinterpret_cast<uintptr_t>(out) & 15u) != 0)
+            e = record_error(KMIP_ERR_INVALID_ARG, "out must be 16-byte aligned");
+        if (e == KMIP_OK) e = plan_fwd(sq, H, Hk, &p);
+        if (e != KMIP_OK) return e;
+        const FwdLayout L = fwd_layout(p, dv);
+        if ((e = check_workspace(workspace, workspace_bytes, L.total)) != KMIP_OK) return e;
+        f.out = out;
+        f.lse = lse;
+        char* ws = reinterpret_cast<char*>(workspace);
+        hipError_t h = kmip::launch_full_fwd(f, p, reinterpret_cast<float*>(ws),
+                                             L.total > 0 ? reinterpret_cast<float*>(ws + L.ml) : nullptr,
+                                             reinterpret_cast<hipStream_t>(stream));
+        return h == hipSuccess ? ok() : hip_fail(h, "full attention launch");
+    });
+}
+
+}  // extern "C"

@@ -1,0 +1,190 @@
+// Shared by the kernels of full softmax attention (full_fwd.hip, full_bwd.hip).
+//
+// All products run as 32 x 32 x 16 matrix instructions on 16-bit operands
+// with float32 sums.  The side a wave keeps (32 rows, "columns" below) is the
+// right operand, held in registers; the other side streams through LDS in
+// tiles of rows and is the left operand, so that a score tile comes out
+// transposed: lane l holds column l % 32 and, in register r, the streamed row
+// (r & 3) + 8 (r >> 2) + 4 (l / 32).  Two properties carry the kernels:
+//   - statistics of a column (maximum, sum, log-sum) are the lane's own and
+//     its partner's (l ^ 32);
+//   - eight consecutive registers, rounded to 16 bits, are the right operand
+//     of the next product over the streamed rows, with the contraction in
+//     the order {0-3, 8-11} (lanes 0-31), {4-7, 12-15} (lanes 32-63) of each 16
+//     rows; the left operand is read from LDS transposed (ds_read_b64_tr_b16:
+//     four rows of one column a lane) in the same order.  No value changes
+//     lanes between the two products.
+//
+// LDS tiles are rows of D 16-bit values; the 16-byte chunk c of row r lies at
+// place c ^ swz(r), which spreads both kinds of reads over the 64 banks
+// (measured: 205 bytes a clock and CU for the plain reads, 256 for the
+// transposed ones, of 256; 16 without the permutation).  Tiles are written by
+// loads that go from memory to LDS directly, 1 KB an instruction; the
+// permutation is applied to the address each lane reads from.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "kmip_device.h"
+#include "full_plan.h"
+
+namespace kmip {
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+#define KMIP_LDS __attribute__((address_space(3)))
+#define KMIP_GLOBAL __attribute__((address_space(1)))
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+struct Bf16 {
+    static __device__ __forceinline__ f32x16 mfma(s16x8 a, s16x8 b, f32x16 c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0,
+                                                       0, 0);
+    }
+    static __device__ __forceinline__ short round(float x) { return __builtin_bit_cast(short, (__bf16)x); }
+    static __device__ __forceinline__ float widen(short x) { return __uint_as_float((uint32_t)(uint16_t)x << 16); }
+};
+
+struct Fp16 {
+    static __device__ __forceinline__ f32x16 mfma(s16x8 a, s16x8 b, f32x16 c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0,
+                                                      0);
+    }
+    static __device__ __forceinline__ short round(float x) { return __builtin_bit_cast(short, (_Float16)x); }
+    static __device__ __forceinline__ float widen(short x) { return (float)__builtin_bit_cast(_Float16, x); }
+};
+
+// Place permutation of a row's 16-byte chunks.  Transposed reads touch 64
+// bytes of eight rows, plain ones 16 bytes of 32: the chunk's bits above 2
+// (64-byte places) follow the row's lowest bits, as far as the row length
+// leaves rows in the same 256 bytes, its low two bits the next ones.
+template <int D>
+__device__ __forceinline__ int swz(int r) {
+    if constexpr (D == 128) return ((r & 3) << 2) | ((r >> 2) & 3);
+    if constexpr (D == 64) return (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
+    if constexpr (D == 32) return (r >> 2) & 3;
+    return (r >> 3) & 1;
+}
+
+__device__ __forceinline__ uint32_t lds_addr(const void* p) {
+    return (uint32_t)(uintptr_t)(const KMIP_LDS char*)p;
+}
+
+__device__ __forceinline__ s16x8 lds_row16(uint32_t a) { return *(const KMIP_LDS s16x8*)(uintptr_t)a; }
+
+__device__ __forceinline__ s16x8 lds_rows_tr(uint32_t a, uint32_t b) {
+    const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((KMIP_LDS s16x4*)(uintptr_t)a);
+    const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((KMIP_LDS s16x4*)(uintptr_t)b);
+    return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
+// This lane's address of the plain left operand: rows R .. R + 31 (R a
+// multiple of 32) of a tile are at + R * 2D, dimensions 16 s .. 16 s + 15 at
+// ^ (32 s).
+template <int D>
+__device__ __forceinline__ uint32_t row_operand(uint32_t tile, int lane) {
+    const int r = lane & 31, c = lane >> 5;
+    return tile + r * 2 * D + ((c ^ swz<D>(r)) << 4);
+}
+
+// This lane's addresses of the transposed left operand (columns 32 t .. 32 t +
+// 31 of the tile as operand rows, tile rows R .. R + 15, R a multiple of 16, as
+// contraction), first and second half: columns at ^ (64 t), rows at + R * 2D.
+template <int D>
+__device__ __forceinline__ void tr_operand(uint32_t (&a)[2], uint32_t tile, int lane) {
+    const int l = lane & 15, g = (lane >> 4) & 1, h = lane >> 5;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int r = 8 * i + 4 * h + (l >> 2);
+        const int c = (D >= 32 ? 2 * g : 0) + ((l >> 1) & 1);
+        a[i] = tile + r * 2 * D + ((c ^ swz<D>(r)) << 4) + (l & 1) * 8;
+    }
+}
+
+// x of this lane and of its partner lane ^ 32, as (lower lane's, upper lane's).
+__device__ __forceinline__ float2 both_halves(float x) {
+    const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return make_float2(__uint_as_float(p[0]), __uint_as_float(p[1]));
+}
+
+// Memory to LDS, 16 bytes a lane: lane l's 16 bytes at base + off go to
+// lds + 16 l (base and lds uniform).
+__device__ __forceinline__ void load_to_lds(uint32_t lds, const char* base, uint32_t off) {
+    __builtin_amdgcn_global_load_lds((const KMIP_GLOBAL void*)(base + off), (KMIP_LDS void*)(uintptr_t)lds, 16, 0, 0);
+}
+
+// All but the last n loads of this wave have ended.
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+
+// All LDS accesses of this wave have ended.
+__device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
+// Every load to LDS and LDS access of this wave has ended, and then of the
+// workgroup's other waves.
+__device__ __forceinline__ void wait_and_sync() {
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
+// Loads tiles of rows of a strided tensor into LDS.  A round of PARTS
+// instructions (one from each of PARTS waves) writes PARTS * 512 / D rows.
+// Columns from `cols` on (there are some when the tensor is narrower than the
+// kernel's width) repeat the row's first chunk: they meet zeros in the other
+// operand, or make output columns that are not stored.
+template <int D, int PARTS>
+struct TileLoad {
+    static constexpr int kPer = 512 / D * PARTS;            // rows of a round
+    static constexpr int kVar = kPer < 16 ? 16 / kPer : 1;  // rounds after which the permutation repeats
+    uint32_t off[kVar];   // this lane's bytes in a round's rows
+    uint32_t row;         // its row among them
+    uint32_t stride;      // bytes between rows
+
+    __device__ __forceinline__ void init(int lane, int part, int32_t cols, uint32_t row_stride) {
+        row = part * (512 / D) + lane / (D / 8);
+        stride = row_stride;
+#pragma unroll
+        for (int v = 0; v < kVar; ++v) {
+            uint32_t c = (uint32_t)(lane & (D / 8 - 1)) ^ (uint32_t)swz<D>((int)row + v * kPer);
+            if ((int32_t)(8 * c) >= cols) c = 0;
+            off[v] = row * stride + 16 * c;
+        }
+    }
+    // ROWS rows from the one at `base` on; those from `left` on are replaced by
+    // row left - 1 (left >= 1), so that no address lies behind the last row.
+    template <int ROWS>
+    __device__ __forceinline__ void issue(uint32_t lds, const char* base, int part, int32_t left) const {
+        static_assert(ROWS % kPer == 0, "whole rounds");
+        constexpr int kRounds = ROWS / kPer;
+        lds += part * 1024;
+        if (left >= ROWS) {
+#pragma unroll
+            for (int i = 0; i < kRounds; ++i)
+                load_to_lds(lds + i * PARTS * 1024, base + (uint64_t)(uint32_t)(i * kPer) * stride, off[i % kVar]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kRounds; ++i) {
+                const uint32_t back = row - (uint32_t)min((int32_t)row + i * kPer, left - 1);
+                load_to_lds(lds + i * PARTS * 1024, base, off[i % kVar] - back * stride);
+            }
+        }
+    }
+};
+
+// ---- jobs (full_plan.h) ----
+// The sequence a job belongs to (uniform over the workgroup).
+__device__ __forceinline__ int seq_of_job(const FullSeqs& s, int32_t job, int lane) {
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < kFullSeqs; i += 64)
+        n += __popcll(__ballot(i + lane < s.count && s.job0[i + lane] <= job));
+    return n - 1;
+}
+
+}  // namespace kmip

@@ -1,0 +1,426 @@
+// Full softmax attention over packed sequences: forward (gfx950).
+//
+// For query row i (a token and head) of a sequence with keys j:
+//   s_ij = q_i . k_j,  out_i = sum_j p_ij v_j,  p_ij = exp(scale s_ij - lse_i),
+//   lse_i = log sum_j exp(scale s_ij),
+// in one pass over the keys with a running maximum m and sum l: a tile's
+// weights are 2^(c (s - m)), c = scale log2 e, and what was summed before a
+// new maximum is multiplied by 2^(c (m_old - m_new)).  The score matrix is
+// never stored.
+//
+// Rows: the query heads that share a key head and the tokens of a sequence
+// form one list, row = token * rep + head in the group, so that a tile of 32
+// rows reads the keys once for all its heads (a single token of 8 grouped heads
+// fills 8 columns of one product instead of one of 8).
+//
+// Two forms:
+//   ROWS = 128: four waves of 32 rows share each tile of keys (two buffers,
+//     one barrier a tile);
+//   ROWS = 32: the four waves hold the same rows and take every fourth block of
+//     32 keys, each with LDS of its own and no barrier, and are joined at the
+//     end.  For few rows.
+// With `split` keys per job, jobs of a row tile take runs of its keys and write
+// partial sums, which full_join_kernel joins in the order of the runs.
+#include "full_common.h"
+
+namespace kmip {
+namespace {
+
+struct FwdArgs {
+    const char *q, *k, *v;
+    uint16_t* out;
+    float* lse;
+    float *part_o, *part_ml;    // split: [job][ROWS][dv] sums, [job][ROWS][2] maximum (times c) and sum
+    int64_t q_row, q_head, k_row, k_head, v_row, v_head;   // bytes between tokens, heads
+    int32_t H, Hk, rep, d, dv, causal, split;
+    float scale;
+    int32_t first_job;          // of the launch, among the call's
+    FullSeqs s;
+};
+
+struct Job {
+    int32_t q_lo, q_len, k_lo, k_len, kv_head, tile, run, runs;
+};
+
+template <int ROWS>
+__device__ __forceinline__ Job find_job(const FwdArgs& a, int32_t job, int lane) {
+    const int s = __builtin_amdgcn_readfirstlane(seq_of_job(a.s, job, lane));
+    Job j;
+    j.q_lo = a.s.q_lo[s];
+    j.q_len = a.s.q_len[s];
+    j.k_lo = a.s.k_lo[s];
+    j.k_len = a.s.k_len[s];
+    j.runs = a.split > 0 && j.k_len > a.split ? (j.k_len + a.split - 1) / a.split : 1;
+    const int32_t tiles = (int32_t)(((int64_t)j.q_len * a.rep + ROWS - 1) / ROWS);
+    // key heads first: with 8 of them (or a divisor) workgroups of one XCD,
+    // which come round robin, share a head's keys in its L2
+    int32_t rest = job - a.s.job0[s];
+    j.kv_head = rest % a.Hk;
+    rest /= a.Hk;
+    j.run = rest % j.runs;
+    // causal: the tiles with the most keys first
+    j.tile = rest / j.runs;
+    if (a.causal) j.tile = tiles - 1 - j.tile;
+    return j;
+}
+
+// A wave's running state: 32 columns of rows, two lanes a column.
+template <typename T, int D>
+struct FwdWave {
+    static constexpr int kT = D < 32 ? 1 : D / 32;   // 32-wide pieces of the value columns
+    s16x8 q[D / 16];
+    f32x16 o[kT];
+    float m, l;     // reference of the weights, sum of this lane's
+    int32_t lim;    // keys this row sees
+
+    // NB blocks of 32 keys from key0 on.
+    template <int NB>
+    __device__ __forceinline__ void step(uint32_t ka, const uint32_t (&va)[2], int32_t key0, int32_t lim_first, float c,
+                                         int lane) {
+        f32x16 s[NB];
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[b][r] = 0.0f;
+#pragma unroll
+            for (int t = 0; t < D / 16; ++t) s[b] = T::mfma(lds_row16((ka ^ (32 * t)) + b * 64 * D), q[t], s[b]);
+        }
+        if (key0 + 32 * NB > lim_first) {
+            const int32_t left = lim - key0 - 4 * (lane >> 5);
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (32 * b + (r & 3) + 8 * (r >> 2) >= left) s[b][r] = -INFINITY;
+        }
+        float top = s[0][0];
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) top = fmaxf(top, s[b][r]);
+        const float2 tops = both_halves(top);
+        top = fmaxf(tops.x, tops.y);
+        // The reference follows the maximum only where a weight would pass 2^8: 16-bit
+        // weights keep their relative precision at any reference.
+        if (__any((top - m) * c > 8.0f)) {
+            const float to = fmaxf(top, m);
+            // (no key seen yet: m and top are -inf, and the factor is that of a sum of nothing)
+            const float f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m - to) * c);
+            m = to;
+            l *= f;
+#pragma unroll
+            for (int t = 0; t < kT; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) o[t][r] *= f;
+        }
+        const float mc = m == -INFINITY ? 0.0f : m * c;
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            float sum = 0.0f;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                s[b][r] = __builtin_amdgcn_exp2f(fmaf(s[b][r], c, -mc));
+                sum += s[b][r];
+            }
+            l += sum;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                s16x8 p;   // rounded to the inputs' type: half a step of each weight, the operand of the product
+#pragma unroll
+                for (int e = 0; e < 8; ++e) p[e] = T::round(s[b][8 * i + e]);
+#pragma unroll
+                for (int t = 0; t < kT; ++t) {
+                    const uint32_t at = (32 * b + 16 * i) * 2 * D;
+                    o[t] = T::mfma(lds_rows_tr((va[0] ^ (64 * t)) + at, (va[1] ^ (64 * t)) + at), p, o[t]);
+                }
+            }
+        }
+    }
+};
+
+template <typename T, int D, int ROWS>
+__global__ __launch_bounds__(256, ROWS == 128 ? 2 : 1) void full_fwd_kernel(const FwdArgs a) {
+    constexpr int kTile = ROWS == 128 ? (D == 16 ? 128 : 64) : 32;   // keys a buffer holds
+    constexpr int kBytes = kTile * 2 * D;                            // of one tensor's buffer
+    constexpr int kWaves = 4, kOwn = ROWS == 128 ? 1 : kWaves;       // buffer sets
+    constexpr int kT = FwdWave<T, D>::kT;
+    __shared__ __attribute__((aligned(1024))) char sh[kOwn * 4 * kBytes];
+    static_assert(ROWS == 128 || kOwn * 4 * kBytes >= 32 * D * 4 * kWaves, "room for the join");
+
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const Job j = find_job<ROWS>(a, blockIdx.x, lane);
+    const int32_t nrows = j.q_len * a.rep;
+    const int32_t row0 = j.tile * ROWS + (ROWS == 128 ? 32 * wave : 0);
+    const int32_t off = j.k_len - j.q_len;
+    auto sees = [&](int32_t row) {   // keys row sees (ascending in row)
+        if (!a.causal) return j.k_len;
+        return max(0, min(row, nrows - 1) / a.rep + off + 1);
+    };
+    const int32_t row = row0 + (lane & 31);
+    const bool live = row < nrows;
+    const int32_t token = min(row, nrows - 1) / a.rep, head = j.kv_head * a.rep + min(row, nrows - 1) % a.rep;
+
+    FwdWave<T, D> w;
+    {
+        const char* qp = a.q + (j.q_lo + (int64_t)token) * a.q_row + head * a.q_head;
+#pragma unroll
+        for (int t = 0; t < D / 16; ++t) {
+            const int col = 16 * t + 8 * (lane >> 5);
+            if (col < a.d)
+                w.q[t] = *reinterpret_cast<const s16x8*>(qp + 2 * col);
+            else
+                w.q[t] = s16x8{};
+        }
+    }
+#pragma unroll
+    for (int t = 0; t < kT; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) w.o[t][r] = 0.0f;
+    w.m = -INFINITY;
+    w.l = 0.0f;
+    w.lim = sees(row);
+
+    const int32_t lo = a.split > 0 ? j.run * a.split : 0;
+    int32_t hi = sees(j.tile * ROWS + ROWS - 1);
+    if (a.split > 0) hi = min(hi, lo + a.split);
+    const int32_t lim_first = sees(row0), lim_last = sees(row0 + 31);
+    const float c = a.scale * kLog2e;
+    const char* kp = a.k + (int64_t)j.k_lo * a.k_row + j.kv_head * a.k_head;
+    const char* vp = a.v + (int64_t)j.k_lo * a.v_row + j.kv_head * a.v_head;
+    const uint32_t base = lds_addr(sh) + (ROWS == 128 ? 0 : wave * 4 * kBytes);   // [buffer][K, V]
+    constexpr int kParts = ROWS == 128 ? kWaves : 1;
+    const int part = ROWS == 128 ? wave : 0;
+    TileLoad<D, kParts> kl, vl;
+    kl.init(lane, part, a.d, (uint32_t)a.k_row);
+    vl.init(lane, part, a.dv, (uint32_t)a.v_row);
+    auto fetch = [&](int32_t key, int buf) {
+        kl.template issue<kTile>(base + buf * 2 * kBytes, kp + (int64_t)key * a.k_row, part, j.k_len - key);
+        vl.template issue<kTile>(base + buf * 2 * kBytes + kBytes, vp + (int64_t)key * a.v_row, part, j.k_len - key);
+    };
+    auto compute = [&](int32_t key, int buf) {
+        const uint32_t ka = row_operand<D>(base + buf * 2 * kBytes, lane);
+        uint32_t va[2];
+        tr_operand<D>(va, base + buf * 2 * kBytes + kBytes, lane);
+        w.template step<kTile / 32>(ka, va, key, lim_first, c, lane);
+    };
+    if constexpr (ROWS == 128) {
+        if (lo < hi) fetch(lo, 0);
+        int buf = 0;
+        for (int32_t key = lo; key < hi; key += kTile, buf ^= 1) {
+            wait_and_sync();
+            if (key + kTile < hi) fetch(key + kTile, buf ^ 1);
+            if (key < lim_last) compute(key, buf);
+        }
+    } else {
+        constexpr int kLoads = 2 * kTile / TileLoad<D, 1>::kPer;
+        int32_t key = lo + 32 * wave;
+        if (key < hi) fetch(key, 0);
+        for (int buf = 0; key < hi; key += 32 * kWaves, buf ^= 1) {
+            if (key + 32 * kWaves < hi) {
+                wait_lds();   // the reads of that buffer
+                fetch(key + 32 * kWaves, buf ^ 1);
+                wait_loads<kLoads>();
+            } else {
+                wait_loads<0>();
+            }
+            compute(key, buf);
+        }
+    }
+
+    const float2 ls = both_halves(w.l);
+    float l = ls.x + ls.y, m = w.m;
+    const float mc = m == -INFINITY ? -INFINITY : m * c;
+    const int h = lane >> 5;
+    const int64_t job = (int64_t)a.first_job + blockIdx.x;
+    if constexpr (ROWS == 128) {
+        if (!live) return;
+        if (j.runs > 1) {
+            float* po = a.part_o + (job * ROWS + (row - j.tile * ROWS)) * a.dv;
+#pragma unroll
+            for (int t = 0; t < kT; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; r += 4) {
+                    const int col = 32 * t + 8 * (r >> 2) + 4 * h;
+                    if (col < a.dv) *reinterpret_cast<f32x4*>(po + col) = f32x4{w.o[t][r], w.o[t][r + 1], w.o[t][r + 2], w.o[t][r + 3]};
+                }
+            if (h == 0) {
+                float* ml = a.part_ml + (job * ROWS + (row - j.tile * ROWS)) * 2;
+                ml[0] = mc;
+                ml[1] = l;
+            }
+            return;
+        }
+        const int64_t at = (j.q_lo + (int64_t)token) * a.H + head;
+        const float f = l > 0.0f ? 1.0f / l : 0.0f;
+#pragma unroll
+        for (int t = 0; t < kT; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+                const int col = 32 * t + 8 * (r >> 2) + 4 * h;
+                if (col < a.dv) {
+                    s16x4 x;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[e] = T::round(w.o[t][r + e] * f);
+                    *reinterpret_cast<s16x4*>(a.out + at * a.dv + col) = x;
+                }
+            }
+        if (h == 0) a.lse[at] = l > 0.0f ? (mc + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+    } else {
+        // The four waves' sums of the same rows: to a common reference, added in
+        // LDS [wave][row][D], stored by columns.
+        float* const so = reinterpret_cast<float*>(sh);
+        __shared__ float sm[kWaves][32], sl[kWaves][32];
+        if (h == 0) {
+            sm[wave][lane] = mc;
+            sl[wave][lane] = l;
+        }
+        wait_and_sync();
+        const int rw = lane & 31;
+        float top = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < kWaves; ++i) top = fmaxf(top, sm[i][rw]);
+        const float f = mc == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mc - top);
+        // rows of D + 4 values would not fit; the columns' groups of four are turned by the row instead
+#pragma unroll
+        for (int t = 0; t < kT; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+                const int g = 8 * t + 2 * (r >> 2) + h;
+                if (4 * g < D)
+                    *reinterpret_cast<f32x4*>(so + (wave * 32 + rw) * D + 4 * ((g ^ rw) & (D / 4 - 1))) =
+                        f32x4{w.o[t][r] * f, w.o[t][r + 1] * f, w.o[t][r + 2] * f, w.o[t][r + 3] * f};
+            }
+        wait_and_sync();
+        for (int i = threadIdx.x; i < 32 * (D / 4); i += 256) {
+            const int rr = i / (D / 4), g = i % (D / 4);
+            const int32_t rowi = j.tile * ROWS + rr;
+            if (rowi >= nrows || 4 * g >= a.dv) continue;
+            f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+            float mm = -INFINITY, ll = 0.0f;
+#pragma unroll
+            for (int u = 0; u < kWaves; ++u) {
+                x += *reinterpret_cast<const f32x4*>(so + (u * 32 + rr) * D + 4 * ((g ^ rr) & (D / 4 - 1)));
+                mm = fmaxf(mm, sm[u][rr]);
+            }
+#pragma unroll
+            for (int u = 0; u < kWaves; ++u)
+                if (sl[u][rr] > 0.0f) ll += sl[u][rr] * __builtin_amdgcn_exp2f(sm[u][rr] - mm);
+            if (j.runs > 1) {
+                *reinterpret_cast<f32x4*>(a.part_o + (job * ROWS + rr) * a.dv + 4 * g) = x;
+                if (g == 0) {
+                    float* ml = a.part_ml + (job * ROWS + rr) * 2;
+                    ml[0] = mm;
+                    ml[1] = ll;
+                }
+                continue;
+            }
+            const int64_t at = (j.q_lo + (int64_t)(rowi / a.rep)) * a.H + j.kv_head * a.rep + rowi % a.rep;
+            const float inv = ll > 0.0f ? 1.0f / ll : 0.0f;
+            s16x4 y;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] = T::round(x[e] * inv);
+            *reinterpret_cast<s16x4*>(a.out + at * a.dv + 4 * g) = y;
+            if (g == 0) a.lse[at] = ll > 0.0f ? (mm + __builtin_amdgcn_logf(ll)) * kLn2 : -INFINITY;
+        }
+    }
+}
+
+// Joins the runs of a row tile's keys: one workgroup a row.  Threads take
+// (run, four columns); the runs' sums are added in the order of the runs
+// within a thread, then over the threads of a column in a fixed order.
+template <typename T, int ROWS>
+__global__ __launch_bounds__(256) void full_join_kernel(const FwdArgs a) {
+    __shared__ f32x4 part[256];
+    __shared__ float wm[4], wl[4];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const Job j = find_job<ROWS>(a, blockIdx.x, lane);
+    if (j.runs == 1 || j.run != 0) return;
+    const int32_t row = j.tile * ROWS + blockIdx.y;
+    if (row >= j.q_len * a.rep) return;
+    const int64_t job = (int64_t)a.first_job + blockIdx.x;   // run 0; run r is r * Hk jobs on
+    const float* ml = a.part_ml + (job * ROWS + blockIdx.y) * 2;
+    const int64_t step = (int64_t)a.Hk * ROWS;
+    float top = -INFINITY, sum = 0.0f;
+    for (int32_t r = threadIdx.x; r < j.runs; r += 256) top = fmaxf(top, ml[r * step * 2]);
+#pragma unroll
+    for (int s = 1; s < 64; s <<= 1) top = fmaxf(top, __shfl_xor(top, s));
+    if (lane == 0) wm[wave] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(wm[0], wm[1]), fmaxf(wm[2], wm[3]));
+    for (int32_t r = threadIdx.x; r < j.runs; r += 256) {
+        const float l = ml[r * step * 2 + 1];
+        if (l > 0.0f) sum += l * __builtin_amdgcn_exp2f(ml[r * step * 2] - top);
+    }
+#pragma unroll
+    for (int s = 1; s < 64; s <<= 1) sum += __shfl_xor(sum, s);
+    if (lane == 0) wl[wave] = sum;
+    const int groups = a.dv / 4, lanes = 256 / groups;   // 4 .. 32 column groups, 64 .. 8 threads each
+    const int g = threadIdx.x % groups, t = threadIdx.x / groups;
+    const float* po = a.part_o + (job * ROWS + blockIdx.y) * a.dv + 4 * g;
+    f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int32_t r = t; r < j.runs; r += lanes) {
+        if (ml[r * step * 2 + 1] > 0.0f)
+            x += __builtin_amdgcn_exp2f(ml[r * step * 2] - top) * *reinterpret_cast<const f32x4*>(po + r * step * a.dv);
+    }
+    part[threadIdx.x] = x;
+    __syncthreads();
+    if (t != 0) return;
+    for (int u = 1; u < lanes; ++u) x += part[u * groups + g];
+    sum = (wl[0] + wl[1]) + (wl[2] + wl[3]);
+    const int64_t at = (j.q_lo + (int64_t)(row / a.rep)) * a.H + j.kv_head * a.rep + row % a.rep;
+    const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+    s16x4 y;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = T::round(x[e] * inv);
+    *reinterpret_cast<s16x4*>(a.out + at * a.dv + 4 * g) = y;
+    if (g == 0) a.lse[at] = sum > 0.0f ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
+}
+
+template <typename T, int D>
+hipError_t launch_fwd(const FullCall& f, const FullPlan& p, float* part_o, float* part_ml, hipStream_t stream) {
+    FwdArgs a{};
+    a.q = reinterpret_cast<const char*>(f.q);
+    a.k = reinterpret_cast<const char*>(f.k);
+    a.v = reinterpret_cast<const char*>(f.v);
+    a.out = reinterpret_cast<uint16_t*>(f.out);
+    a.lse = f.lse;
+    a.part_o = part_o;
+    a.part_ml = part_ml;
+    a.q_row = 2 * f.q_row, a.q_head = 2 * f.q_head;
+    a.k_row = 2 * f.k_row, a.k_head = 2 * f.k_head;
+    a.v_row = 2 * f.v_row, a.v_head = 2 * f.v_head;
+    a.H = f.H, a.Hk = f.Hk, a.rep = f.H / f.Hk, a.d = f.d, a.dv = f.dv, a.causal = f.causal;
+    a.split = p.split;
+    a.scale = f.scale;
+    for (const FullLaunch& l : p.launches) {
+        a.s = l.seqs;
+        a.first_job = l.first_job;
+        if (p.rows == 128)
+            hipLaunchKernelGGL((full_fwd_kernel<T, D, 128>), dim3(l.jobs), dim3(256), 0, stream, a);
+        else
+            hipLaunchKernelGGL((full_fwd_kernel<T, D, 32>), dim3(l.jobs), dim3(256), 0, stream, a);
+        hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        if (l.split_rows > 0) {
+            hipLaunchKernelGGL((full_join_kernel<T, 32>), dim3(l.jobs, l.split_rows), dim3(256), 0, stream, a);
+            if ((e = hipGetLastError()) != hipSuccess) return e;
+        }
+    }
+    return hipSuccess;
+}
+
+}  // namespace
+
+hipError_t launch_full_fwd(const FullCall& f, const FullPlan& p, float* part_o, float* part_ml, hipStream_t stream) {
+    const int32_t w = f.d > f.dv ? f.d : f.dv;
+#define KMIP_FULL_FWD(D) \
+    if (w == D) return f.fp16 ? launch_fwd<Fp16, D>(f, p, part_o, part_ml, stream) : launch_fwd<Bf16, D>(f, p, part_o, part_ml, stream);
+    KMIP_FULL_FWD(16)
+    KMIP_FULL_FWD(32)
+    KMIP_FULL_FWD(64)
+    KMIP_FULL_FWD(128)
+#undef KMIP_FULL_FWD
+    return hipErrorInvalidValue;
+}
+
+}  // namespace kmip
