@@ -352,6 +352,32 @@ kmip_status_t kmip_full_fwd(const void* Q, const void* K, const void* V, int32_t
                             float scale, int32_t causal, void* out, float* lse, void* workspace, size_t workspace_bytes,
                             void* stream);
 
+/*
+ * Backward of kmip_full_fwd.  With p_ij recomputed from Q, K and lse:
+ *   D_i = dOut_i . out_i,  g_ij = p_ij (dOut_i . v_j - D_i),
+ *   dQ_i = scale sum_j g_ij k_j,  dK_j = scale sum_i g_ij q_i,
+ *   dV_j = sum_i p_ij dOut_i,
+ * the last two over the queries of every head that reads key head of j.
+ *   in:  the forward's arguments; dOut [Nq, H, dv] of the same type; out and
+ *        lse as the forward wrote them.  strides: HOST int64 [8], those of
+ *        kmip_full_fwd and then dOut's two, or NULL: contiguous.
+ *   out: dQ [Nq, H, d], dK [Nk, Hk, d], dV [Nk, Hk, dv] of the inputs' type,
+ *        contiguous, overwritten whole: rows of a slot behind its keys in use,
+ *        and keys that no query sees, get 0.
+ *   p and g are rounded to the inputs' type for the products; every sum is in
+ *   float32 and has one owner, so results are the same from call to call.
+ *   float16: a g_ij beyond 65504 is an infinity.
+ *   workspace: kmip_full_bwd_workspace_size() bytes, 256-byte aligned.
+ */
+size_t kmip_full_bwd_workspace_size(const int32_t* q_offsets, const int32_t* k_offsets, const int32_t* k_lengths,
+                                    int32_t num_seqs, int64_t Nq, int64_t Nk, int32_t H, int32_t Hk, int32_t d,
+                                    int32_t dv);
+kmip_status_t kmip_full_bwd(const void* Q, const void* K, const void* V, const void* dOut, const void* out,
+                            const float* lse, int32_t dtype, const int64_t* strides, const int32_t* q_offsets,
+                            const int32_t* k_offsets, const int32_t* k_lengths, int32_t num_seqs, int64_t Nq, int64_t Nk,
+                            int32_t H, int32_t Hk, int32_t d, int32_t dv, float scale, int32_t causal, void* dQ, void* dK,
+                            void* dV, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Static description of a status code. */
 const char* kmip_status_string(kmip_status_t status);
 

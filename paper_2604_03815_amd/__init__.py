@@ -24,7 +24,8 @@ from ._lib import KmipError, MAX_K, MAX_K_WIDE, NOALLOC_SCRATCH_BYTES, check, lo
 __all__ = [
     "KmipError", "MAX_K", "MAX_K_WIDE", "NOALLOC_SCRATCH_BYTES", "topk", "topk_prefilter", "topk_prefilter_workspace_size", "attend", "fwd", "fwd_noalloc", "bwd",
     "attention", "topk_workspace_size", "bwd_workspace_size", "Workspace", "load", "KMIPAttention",
-    "linear_k_schedule", "full_fwd", "full_fwd_workspace_size",
+    "linear_k_schedule", "full_fwd", "full_fwd_workspace_size", "full_bwd", "full_bwd_workspace_size",
+    "full_attention",
 ]
 
 
@@ -352,5 +353,5 @@ def _attention_function():
     return _Attention
 
 
-from .full import full_fwd, full_fwd_workspace_size  # noqa: E402
+from .full import full_attention, full_bwd, full_bwd_workspace_size, full_fwd, full_fwd_workspace_size  # noqa: E402
 from .layer import KMIPAttention, linear_k_schedule  # noqa: E402

@@ -24,7 +24,7 @@ kmip_status_t hip_fail(hipError_t e, const char* what) {
 }
 
 struct Seq {
-    int32_t q_lo, q_len, k_lo, k_len;
+    int32_t q_lo, q_len, k_lo, k_len, k_slot;
 };
 
 // Where the sequences lie; NULL offsets: see include/kmip.h.
@@ -34,9 +34,10 @@ struct Sequences {
     int64_t Nq, Nk;
 
     Seq at(int32_t g) const {
-        if (q == nullptr) return Seq{0, (int32_t)Nq, 0, len != nullptr ? len[0] : (int32_t)Nk};
+        if (q == nullptr) return Seq{0, (int32_t)Nq, 0, len != nullptr ? len[0] : (int32_t)Nk, (int32_t)Nk};
         const int32_t* ko = k != nullptr ? k : q;
-        return Seq{q[g], q[g + 1] - q[g], ko[g], len != nullptr ? len[g] : ko[g + 1] - ko[g]};
+        const int32_t slot = ko[g + 1] - ko[g];
+        return Seq{q[g], q[g + 1] - q[g], ko[g], len != nullptr ? len[g] : slot, slot};
     }
 };
 
@@ -97,7 +98,7 @@ kmip_status_t cut(std::vector<Seq>& seqs, const Jobs& jobs_of, FullPlan* p) {
         int64_t jobs = 0;
         for (size_t i = 0; i < n; ++i) {
             const Seq& s = seqs[first + i];
-            l.seqs.q_lo[i] = s.q_lo, l.seqs.q_len[i] = s.q_len, l.seqs.k_lo[i] = s.k_lo, l.seqs.k_len[i] = s.k_len;
+            l.seqs.q_lo[i] = s.q_lo, l.seqs.q_len[i] = s.q_len, l.seqs.k_lo[i] = s.k_lo, l.seqs.k_len[i] = s.k_len, l.seqs.k_slot[i] = s.k_slot;
             l.seqs.job0[i] = (int32_t)jobs;
             jobs += jobs_of(s);
             if (p->jobs + jobs >= (int64_t(1) << 31) - 1) return record_error(KMIP_ERR_INVALID_ARG, "too many rows and key runs for one call");
@@ -143,6 +144,27 @@ kmip_status_t plan_fwd(const Sequences& sq, int32_t H, int32_t Hk, FullPlan* p) 
                 if (l.seqs.k_len[i] > split)
                     l.split_rows = std::max<int32_t>(l.split_rows, (int32_t)std::min<int64_t>(32, l.seqs.q_len[i] * rep));
     return KMIP_OK;
+}
+
+// The backward's jobs: row tiles for dQ, key tiles for dK and dV (of every slot,
+// since rows without a gradient are written too).
+kmip_status_t plan_bwd(const Sequences& sq, int32_t H, int32_t Hk, FullPlan* dq, FullPlan* dkv) {
+    const int64_t rep = H / Hk;
+    std::vector<Seq> rows, keys;
+    int64_t nrows = 0, nkeys = 0;
+    for (int32_t g = 0; g < sq.count; ++g) {
+        const Seq s = sq.at(g);
+        if (s.q_len > 0) rows.push_back(s);
+        if (s.k_slot > 0) keys.push_back(s);
+        nrows += s.q_len * rep * Hk;
+        nkeys += (int64_t)s.k_slot * Hk;
+    }
+    dq->rows = nrows >= 256 * 128 ? 128 : 32;
+    dkv->rows = nkeys >= 256 * 128 ? 128 : 32;
+    const int32_t R = dq->rows, S = dkv->rows;
+    kmip_status_t e = cut(rows, [=](const Seq& s) { return (s.q_len * rep + R - 1) / R * Hk; }, dq);
+    if (e != KMIP_OK) return e;
+    return cut(keys, [=](const Seq& s) { return ((int64_t)s.k_slot + S - 1) / S * Hk; }, dkv);
 }
 
 // Workspace of the forward: the runs' sums, then their maxima and sums of weights.
@@ -247,6 +269,42 @@ kmip_status_t kmip_full_fwd(const void* Q, const void* K, const void* V, int32_t
                                              L.total > 0 ? reinterpret_cast<float*>(ws + L.ml) : nullptr,
                                              reinterpret_cast<hipStream_t>(stream));
         return h == hipSuccess ? ok() : hip_fail(h, "full attention launch");
+    });
+}
+
+size_t kmip_full_bwd_workspace_size(const int32_t* q_offsets, const int32_t* k_offsets, const int32_t* k_lengths,
+                                    int32_t num_seqs, int64_t Nq, int64_t Nk, int32_t H, int32_t Hk, int32_t d, int32_t dv) {
+    Sequences sq;
+    if (check_call(q_offsets, k_offsets, k_lengths, num_seqs, Nq, Nk, H, Hk, d, dv, &sq) != KMIP_OK) return 0;
+    return align_up((size_t)Nq * H * sizeof(float));
+}
+
+kmip_status_t kmip_full_bwd(const void* Q, const void* K, const void* V, const void* dOut, const void* out,
+                            const float* lse, int32_t dtype, const int64_t* strides, const int32_t* q_offsets,
+                            const int32_t* k_offsets, const int32_t* k_lengths, int32_t num_seqs, int64_t Nq, int64_t Nk,
+                            int32_t H, int32_t Hk, int32_t d, int32_t dv, float scale, int32_t causal, void* dQ, void* dK,
+                            void* dV, void* workspace, size_t workspace_bytes, void* stream) {
+    return guarded([&]() {
+        Sequences sq;
+        FullCall f;
+        FullPlan dq, dkv;
+        kmip_status_t e = check_call(q_offsets, k_offsets, k_lengths, num_seqs, Nq, Nk, H, Hk, d, dv, &sq);
+        if (e == KMIP_OK && ((Nq > 0 && (!Q || !dOut || !out || !lse || !dQ)) || (Nk > 0 && (!K || !V || !dK || !dV))))
+            e = record_error(KMIP_ERR_INVALID_ARG, "null buffer passed to kmip_full_bwd");
+        if (e == KMIP_OK) e = fill_call(Q, K, V, dtype, strides, Nq, Nk, H, Hk, d, dv, scale, causal, &f);
+        if (e != KMIP_OK) return e;
+        if (strides != nullptr) f.do_row = strides[6], f.do_head = strides[7];
+        if (Nq > 0) e = check_strides("dOut", dOut, f.do_row, f.do_head);
+        for (const void* p : {out, static_cast<const void*>(dQ), static_cast<const void*>(dK), static_cast<const void*>(dV)})
+            if (e == KMIP_OK && (reinterpret_cast<uintptr_t>(p) & 15u) != 0)
+                e = record_error(KMIP_ERR_INVALID_ARG, "out, dQ, dK and dV must be 16-byte aligned");
+        if (e == KMIP_OK) e = check_workspace(workspace, workspace_bytes, align_up((size_t)Nq * H * sizeof(float)));
+        if (e == KMIP_OK) e = plan_bwd(sq, H, Hk, &dq, &dkv);
+        if (e != KMIP_OK) return e;
+        f.dout = dOut, f.out_in = out, f.lse_in = lse;
+        f.dq = dQ, f.dk = dK, f.dv_out = dV;
+        hipError_t h = kmip::launch_full_bwd(f, dq, dkv, reinterpret_cast<float*>(workspace), reinterpret_cast<hipStream_t>(stream));
+        return h == hipSuccess ? ok() : hip_fail(h, "full attention backward launch");
     });
 }
 

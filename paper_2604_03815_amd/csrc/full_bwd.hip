@@ -1,0 +1,417 @@
+// Full softmax attention over packed sequences: backward (gfx950).
+//
+// With p_ij = exp(scale s_ij - lse_i) recomputed from the forward's lse:
+//   D_i = dout_i . out_i,  dp_ij = dout_i . v_j,  g_ij = p_ij (dp_ij - D_i),
+//   dq_i = scale sum_j g_ij k_j,  dk_j = scale sum_i g_ij q_i,  dv_j = sum_i p_ij dout_i.
+// Two kernels, so that every sum has one owner and no atomics are needed
+// (results are the same from call to call):
+//   full_dq_kernel   keeps rows (as the forward does: tokens and the heads that
+//                    share a key head) and streams keys: s, dp, then dq; it also
+//                    forms D of its rows and leaves it for the other kernel;
+//   full_dkv_kernel  keeps keys and streams the tokens of one head after the
+//                    other of its group: s, dp, then dv and dk.
+// They form s and dp twice, seven products where one pass with atomics would
+// need five.  Forms for many and for few kept rows as in the forward.
+#include "full_common.h"
+
+namespace kmip {
+namespace {
+
+struct BwdArgs {
+    const char *q, *k, *v, *dout;
+    const uint16_t* out;
+    const float* lse;
+    float* D;
+    uint16_t *dq, *dk, *dv_out;
+    int64_t q_row, q_head, k_row, k_head, v_row, v_head, do_row, do_head;   // bytes between tokens, heads
+    int32_t H, Hk, rep, d, dv, causal;
+    float scale;
+    FullSeqs s;
+};
+
+template <typename T, int D, int ROWS>
+__global__ __launch_bounds__(256, ROWS == 128 ? 2 : 1) void full_dq_kernel(const BwdArgs a) {
+    constexpr int kTile = ROWS == 128 ? (D == 16 ? 128 : 64) : 32;
+    constexpr int kBytes = kTile * 2 * D;
+    constexpr int kWaves = 4, kOwn = ROWS == 128 ? 1 : kWaves;
+    constexpr int kT = D < 32 ? 1 : D / 32;
+    __shared__ __attribute__((aligned(1024))) char sh[kOwn * 4 * kBytes];
+
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const RowJob j = row_job<ROWS>(a.s, a.Hk, a.rep, a.causal, 0, blockIdx.x, lane);
+    const int32_t nrows = j.q_len * a.rep;
+    const int32_t row0 = j.tile * ROWS + (ROWS == 128 ? 32 * wave : 0);
+    const int32_t off = j.k_len - j.q_len;
+    auto sees = [&](int32_t row) {
+        if (!a.causal) return j.k_len;
+        return max(0, min(row, nrows - 1) / a.rep + off + 1);
+    };
+    const int32_t row = row0 + (lane & 31);
+    const bool live = row < nrows;
+    const int32_t token = min(row, nrows - 1) / a.rep, head = j.kv_head * a.rep + min(row, nrows - 1) % a.rep;
+    const int64_t at = (j.q_lo + (int64_t)token) * a.H + head;
+
+    s16x8 q[D / 16], g[D / 16];
+    load_columns<D>(q, a.q + (j.q_lo + (int64_t)token) * a.q_row + head * a.q_head, a.d, lane);
+    load_columns<D>(g, a.dout + (j.q_lo + (int64_t)token) * a.do_row + head * a.do_head, a.dv, lane);
+    float di = 0.0f;
+    {
+        s16x8 o[D / 16];
+        load_columns<D>(o, reinterpret_cast<const char*>(a.out + at * a.dv), a.dv, lane);
+#pragma unroll
+        for (int t = 0; t < D / 16; ++t)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) di = fmaf(T::widen(g[t][e]), T::widen(o[t][e]), di);
+        const float2 ds = both_halves(di);
+        di = ds.x + ds.y;
+    }
+    if (live && lane < 32 && (ROWS == 128 || wave == 0)) a.D[at] = di;
+    const float lse = a.lse[at];
+    // a row that sees no key: every weight 0
+    const float lse2 = lse == -INFINITY ? INFINITY : lse * kLog2e;
+    const float c = a.scale * kLog2e;
+    const int32_t lim = sees(row), lim_first = sees(row0), lim_last = sees(row0 + 31), hi = sees(j.tile * ROWS + ROWS - 1);
+
+    const char* kp = a.k + (int64_t)j.k_lo * a.k_row + j.kv_head * a.k_head;
+    const char* vp = a.v + (int64_t)j.k_lo * a.v_row + j.kv_head * a.v_head;
+    const uint32_t base = lds_addr(sh) + (ROWS == 128 ? 0 : wave * 4 * kBytes);
+    constexpr int kParts = ROWS == 128 ? kWaves : 1;
+    const int part = ROWS == 128 ? wave : 0;
+    TileLoad<D, kParts> kl, vl;
+    kl.init(lane, part, a.d, (uint32_t)a.k_row);
+    vl.init(lane, part, a.dv, (uint32_t)a.v_row);
+    auto fetch = [&](int32_t key, int buf) {
+        kl.template issue<kTile>(base + buf * 2 * kBytes, kp + (int64_t)key * a.k_row, part, j.k_len - key);
+        vl.template issue<kTile>(base + buf * 2 * kBytes + kBytes, vp + (int64_t)key * a.v_row, part, j.k_len - key);
+    };
+    f32x16 acc[kT];
+#pragma unroll
+    for (int t = 0; t < kT; ++t) clear(acc[t]);
+    auto compute = [&](int32_t key0, int buf) {
+        const uint32_t kt = base + buf * 2 * kBytes;
+        const uint32_t ka = row_operand<D>(kt, lane), va = row_operand<D>(kt + kBytes, lane);
+        uint32_t ta[2];
+        tr_operand<D>(ta, kt, lane);
+#pragma unroll
+        for (int b = 0; b < kTile / 32; ++b) {
+            f32x16 s, dp;
+            clear(s);
+            clear(dp);
+#pragma unroll
+            for (int t = 0; t < D / 16; ++t) s = T::mfma(lds_row16((ka ^ (32 * t)) + b * 64 * D), q[t], s);
+#pragma unroll
+            for (int t = 0; t < D / 16; ++t) dp = T::mfma(lds_row16((va ^ (32 * t)) + b * 64 * D), g[t], dp);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], c, -lse2)) * (dp[r] - di);
+            if (key0 + 32 * b + 32 > lim_first) {
+                const int32_t left = lim - key0 - 32 * b - 4 * (lane >> 5);
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if ((r & 3) + 8 * (r >> 2) >= left) s[r] = 0.0f;
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const s16x8 p = round8<T>(s, i);   // rounded to the inputs' type, the operand of the product
+#pragma unroll
+                for (int t = 0; t < kT; ++t) {
+                    const uint32_t o = (32 * b + 16 * i) * 2 * D;
+                    acc[t] = T::mfma(lds_rows_tr((ta[0] ^ (64 * t)) + o, (ta[1] ^ (64 * t)) + o), p, acc[t]);
+                }
+            }
+        }
+    };
+    if constexpr (ROWS == 128) {
+        if (hi > 0) fetch(0, 0);
+        int buf = 0;
+        for (int32_t key = 0; key < hi; key += kTile, buf ^= 1) {
+            wait_and_sync();
+            if (key + kTile < hi) fetch(key + kTile, buf ^ 1);
+            if (key < lim_last) compute(key, buf);
+        }
+        if (!live) return;
+#pragma unroll
+        for (int t = 0; t < kT; ++t) store_piece<T>(a.dq + at * a.d, acc[t], t, a.scale, a.d, lane);
+    } else {
+        constexpr int kLoads = 2 * kTile / TileLoad<D, 1>::kPer;
+        int32_t key = 32 * wave;
+        if (key < hi) fetch(key, 0);
+        for (int buf = 0; key < hi; key += 32 * kWaves, buf ^= 1) {
+            if (key + 32 * kWaves < hi) {
+                wait_lds();   // the reads of that buffer
+                fetch(key + 32 * kWaves, buf ^ 1);
+                wait_loads<kLoads>();
+            } else {
+                wait_loads<0>();
+            }
+            compute(key, buf);
+        }
+        // the four waves' sums, in their order
+        wait_and_sync();
+        float* const so = reinterpret_cast<float*>(sh);
+#pragma unroll
+        for (int t = 0; t < kT; ++t) put_piece<D>(so + wave * 32 * D, acc[t], t, a.scale, lane);
+        wait_and_sync();
+        for (int i = threadIdx.x; i < 32 * (D / 4); i += 256) {
+            const int rr = i / (D / 4), gg = i % (D / 4);
+            const int32_t rowi = j.tile * ROWS + rr;
+            if (rowi >= nrows || 4 * gg >= a.d) continue;
+            f32x4 x = get_piece<D>(so, rr, gg);
+#pragma unroll
+            for (int u = 1; u < kWaves; ++u) x += get_piece<D>(so + u * 32 * D, rr, gg);
+            const int64_t to = (j.q_lo + (int64_t)(rowi / a.rep)) * a.H + j.kv_head * a.rep + rowi % a.rep;
+            s16x4 y;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] = T::round(x[e]);
+            *reinterpret_cast<s16x4*>(a.dq + to * a.d + 4 * gg) = y;
+        }
+    }
+}
+
+template <typename T, int D, int KEYS>
+__global__ __launch_bounds__(256, KEYS == 128 && D < 128 ? 2 : 1) void full_dkv_kernel(const BwdArgs a) {
+    constexpr int kTile = KEYS == 128 ? (D == 16 ? 128 : 64) : 32;   // tokens a buffer holds
+    constexpr int kBytes = kTile * 2 * D;
+    constexpr int kWaves = 4, kOwn = KEYS == 128 ? 1 : kWaves;
+    constexpr int kT = D < 32 ? 1 : D / 32;
+    __shared__ __attribute__((aligned(1024))) char sh[kOwn * 4 * kBytes];       // [buffer][Q, dout]
+    __shared__ __attribute__((aligned(16))) float st[kOwn][2][2][kTile];       // [buffer][lse log2 e, D]
+
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int sq = __builtin_amdgcn_readfirstlane(seq_of_job(a.s, blockIdx.x, lane));
+    const int32_t q_lo = a.s.q_lo[sq], q_len = a.s.q_len[sq], k_lo = a.s.k_lo[sq], k_len = a.s.k_len[sq], slot = a.s.k_slot[sq];
+    const int32_t kv_head = (blockIdx.x - a.s.job0[sq]) % a.Hk, tile = (blockIdx.x - a.s.job0[sq]) / a.Hk;
+    const int32_t off = k_len - q_len;
+    const int32_t tile_lo = tile * KEYS;                       // keys from here on
+    const int32_t key0 = tile_lo + (KEYS == 128 ? 32 * wave : 0), key = key0 + (lane & 31);
+    const int64_t key_at = min(key, max(k_len, 1) - 1);
+    s16x8 k[D / 16], v[D / 16];
+    if (k_len > 0) {
+        load_columns<D>(k, a.k + (k_lo + key_at) * a.k_row + kv_head * a.k_head, a.d, lane);
+        load_columns<D>(v, a.v + (k_lo + key_at) * a.v_row + kv_head * a.v_head, a.dv, lane);
+    } else {
+#pragma unroll
+        for (int t = 0; t < D / 16; ++t) k[t] = v[t] = s16x8{};
+    }
+    // the first token that sees the tile, and its first and last key of this wave
+    const int32_t t_lo = tile_lo >= k_len ? q_len : a.causal ? max(0, tile_lo - off) : 0;
+    const int32_t t_wave = a.causal ? key0 - off : 0, t_all = a.causal ? key0 + 31 - off : 0;
+    const float c = a.scale * kLog2e;
+
+    f32x16 dk[kT], dv[kT];
+#pragma unroll
+    for (int t = 0; t < kT; ++t) clear(dk[t]), clear(dv[t]);
+    const uint32_t base = lds_addr(sh) + (KEYS == 128 ? 0 : wave * 4 * kBytes);
+    float(*const stats)[2][kTile] = st[KEYS == 128 ? 0 : wave];
+    constexpr int kParts = KEYS == 128 ? kWaves : 1;
+    const int part = KEYS == 128 ? wave : 0;
+    TileLoad<D, kParts> ql, gl;
+    ql.init(lane, part, a.d, (uint32_t)a.q_row);
+    gl.init(lane, part, a.dv, (uint32_t)a.do_row);
+    auto fetch = [&](int32_t hr, int32_t tok, int buf) {
+        const int32_t head = kv_head * a.rep + hr;
+        ql.template issue<kTile>(base + buf * 2 * kBytes, a.q + (q_lo + (int64_t)tok) * a.q_row + head * a.q_head, part,
+                                 q_len - tok);
+        gl.template issue<kTile>(base + buf * 2 * kBytes + kBytes, a.dout + (q_lo + (int64_t)tok) * a.do_row + head * a.do_head,
+                                 part, q_len - tok);
+    };
+    // one token's lse log2 e and D; a token behind the last, or one that sees no
+    // key, has weights 0 through an infinite lse
+    auto stat = [&](int32_t hr, int32_t tok, int i) {
+        float2 x = make_float2(INFINITY, 0.0f);
+        if (tok + i < q_len) {
+            const int64_t at = (q_lo + (int64_t)(tok + i)) * a.H + kv_head * a.rep + hr;
+            const float lse = a.lse[at], di = a.D[at];
+            if (lse != -INFINITY) x = make_float2(lse * kLog2e, di);
+        }
+        return x;
+    };
+    auto compute = [&](int32_t tok, int buf) {
+        const uint32_t qt = base + buf * 2 * kBytes;
+        const uint32_t qa = row_operand<D>(qt, lane), ga = row_operand<D>(qt + kBytes, lane);
+        uint32_t tq[2], tg[2];
+        tr_operand<D>(tq, qt, lane);
+        tr_operand<D>(tg, qt + kBytes, lane);
+#pragma unroll
+        for (int b = 0; b < kTile / 32; ++b) {
+            f32x16 s, dp;
+            clear(s);
+            clear(dp);
+#pragma unroll
+            for (int t = 0; t < D / 16; ++t) s = T::mfma(lds_row16((qa ^ (32 * t)) + b * 64 * D), k[t], s);
+#pragma unroll
+            for (int t = 0; t < D / 16; ++t) dp = T::mfma(lds_row16((ga ^ (32 * t)) + b * 64 * D), v[t], dp);
+            const float* sb = &stats[buf][0][32 * b + 4 * (lane >> 5)];
+            const bool edge = tok + 32 * b < t_all;
+            const int32_t from = a.causal ? key - off - tok - 32 * b - 4 * (lane >> 5) : 0;   // first row that sees the key
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+                const f32x4 l = *reinterpret_cast<const f32x4*>(sb + 2 * r), di = *reinterpret_cast<const f32x4*>(sb + kTile + 2 * r);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float p = __builtin_amdgcn_exp2f(fmaf(s[r + e], c, -l[e]));
+                    float x = p * (dp[r + e] - di[e]);
+                    if (edge && e + 2 * r < from) p = 0.0f, x = 0.0f;
+                    s[r + e] = p;
+                    dp[r + e] = x;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const s16x8 p = round8<T>(s, i), x = round8<T>(dp, i);   // rounded, the operands of the products
+#pragma unroll
+                for (int t = 0; t < kT; ++t) {
+                    const uint32_t o = (32 * b + 16 * i) * 2 * D;
+                    dv[t] = T::mfma(lds_rows_tr((tg[0] ^ (64 * t)) + o, (tg[1] ^ (64 * t)) + o), p, dv[t]);
+                    dk[t] = T::mfma(lds_rows_tr((tq[0] ^ (64 * t)) + o, (tq[1] ^ (64 * t)) + o), x, dk[t]);
+                }
+            }
+        }
+    };
+
+    // tiles: rep heads of `per` tiles each
+    const int32_t per = (q_len - t_lo + kTile - 1) / kTile;
+    const int32_t n = t_lo < q_len ? per * a.rep : 0;
+    if constexpr (KEYS == 128) {
+        int32_t hr = 0, tok = t_lo;
+        if (n > 0) {
+            fetch(0, tok, 0);
+            if (threadIdx.x < kTile) {
+                const float2 x = stat(0, tok, threadIdx.x);
+                stats[0][0][threadIdx.x] = x.x;
+                stats[0][1][threadIdx.x] = x.y;
+            }
+        }
+        for (int32_t i = 0; i < n; ++i) {
+            const int buf = i & 1;
+            const int32_t now = tok;
+            wait_and_sync();
+            float2 x = make_float2(0.0f, 0.0f);
+            if (i + 1 < n) {
+                tok += kTile;
+                if (tok >= q_len) tok = t_lo, ++hr;
+                if (threadIdx.x < kTile) x = stat(hr, tok, threadIdx.x);
+                fetch(hr, tok, buf ^ 1);
+            }
+            if (now + kTile > t_wave) compute(now, buf);
+            if (i + 1 < n && threadIdx.x < kTile) {
+                stats[buf ^ 1][0][threadIdx.x] = x.x;
+                stats[buf ^ 1][1][threadIdx.x] = x.y;
+            }
+        }
+        if (key >= slot) return;
+        const int64_t at = (k_lo + (int64_t)key) * a.Hk + kv_head;
+        // rows behind the keys in use have no gradient
+        const bool used = key < k_len;
+#pragma unroll
+        for (int t = 0; t < kT; ++t) {
+            if (!used) clear(dk[t]), clear(dv[t]);
+            store_piece<T>(a.dk + at * a.d, dk[t], t, a.scale, a.d, lane);
+            store_piece<T>(a.dv_out + at * a.dv, dv[t], t, 1.0f, a.dv, lane);
+        }
+    } else {
+        constexpr int kLoads = 2 * kTile / TileLoad<D, 1>::kPer;
+        auto place = [&](int32_t i, int32_t* hr, int32_t* tok) {
+            *hr = i / per;
+            *tok = t_lo + (i % per) * kTile;
+        };
+        int32_t hr = 0, tok = 0;
+        float2 x = make_float2(0.0f, 0.0f);
+        if (wave < n) {
+            place(wave, &hr, &tok);
+            x = stat(hr, tok, lane & 31);
+            fetch(hr, tok, 0);
+        }
+        for (int32_t i = wave, buf = 0; i < n; i += kWaves, buf ^= 1) {
+            const int32_t now = tok;
+            if (lane < 32) stats[buf][0][lane] = x.x, stats[buf][1][lane] = x.y;
+            wait_lds();   // the reads of the other buffer, and this write
+            if (i + kWaves < n) {
+                place(i + kWaves, &hr, &tok);
+                x = stat(hr, tok, lane & 31);
+                fetch(hr, tok, buf ^ 1);
+                wait_loads<kLoads>();
+            } else {
+                wait_loads<0>();
+            }
+            compute(now, buf);
+        }
+        // the four waves' sums, in their order: dK, then dV
+        float* const so = reinterpret_cast<float*>(sh);
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+            const int32_t width = w == 0 ? a.d : a.dv;
+            wait_and_sync();
+#pragma unroll
+            for (int t = 0; t < kT; ++t) put_piece<D>(so + wave * 32 * D, w == 0 ? dk[t] : dv[t], t, w == 0 ? a.scale : 1.0f, lane);
+            wait_and_sync();
+            for (int i = threadIdx.x; i < 32 * (D / 4); i += 256) {
+                const int rr = i / (D / 4), gg = i % (D / 4);
+                if (tile_lo + rr >= slot || 4 * gg >= width) continue;
+                f32x4 y = get_piece<D>(so, rr, gg);
+#pragma unroll
+                for (int u = 1; u < kWaves; ++u) y += get_piece<D>(so + u * 32 * D, rr, gg);
+                s16x4 z;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) z[e] = T::round(tile_lo + rr < k_len ? y[e] : 0.0f);
+                uint16_t* to = w == 0 ? a.dk : a.dv_out;
+                *reinterpret_cast<s16x4*>(to + ((k_lo + (int64_t)(tile_lo + rr)) * a.Hk + kv_head) * width + 4 * gg) = z;
+            }
+        }
+    }
+}
+
+template <typename T, int D>
+hipError_t launch_bwd(const FullCall& f, const FullPlan& dq, const FullPlan& dkv, float* Dv, hipStream_t stream) {
+    BwdArgs a{};
+    a.q = reinterpret_cast<const char*>(f.q);
+    a.k = reinterpret_cast<const char*>(f.k);
+    a.v = reinterpret_cast<const char*>(f.v);
+    a.dout = reinterpret_cast<const char*>(f.dout);
+    a.out = reinterpret_cast<const uint16_t*>(f.out_in);
+    a.lse = f.lse_in;
+    a.D = Dv;
+    a.dq = reinterpret_cast<uint16_t*>(f.dq);
+    a.dk = reinterpret_cast<uint16_t*>(f.dk);
+    a.dv_out = reinterpret_cast<uint16_t*>(f.dv_out);
+    a.q_row = 2 * f.q_row, a.q_head = 2 * f.q_head;
+    a.k_row = 2 * f.k_row, a.k_head = 2 * f.k_head;
+    a.v_row = 2 * f.v_row, a.v_head = 2 * f.v_head;
+    a.do_row = 2 * f.do_row, a.do_head = 2 * f.do_head;
+    a.H = f.H, a.Hk = f.Hk, a.rep = f.H / f.Hk, a.d = f.d, a.dv = f.dv, a.causal = f.causal;
+    a.scale = f.scale;
+    for (const FullLaunch& l : dq.launches) {
+        a.s = l.seqs;
+        if (dq.rows == 128)
+            hipLaunchKernelGGL((full_dq_kernel<T, D, 128>), dim3(l.jobs), dim3(256), 0, stream, a);
+        else
+            hipLaunchKernelGGL((full_dq_kernel<T, D, 32>), dim3(l.jobs), dim3(256), 0, stream, a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    for (const FullLaunch& l : dkv.launches) {
+        a.s = l.seqs;
+        if (dkv.rows == 128)
+            hipLaunchKernelGGL((full_dkv_kernel<T, D, 128>), dim3(l.jobs), dim3(256), 0, stream, a);
+        else
+            hipLaunchKernelGGL((full_dkv_kernel<T, D, 32>), dim3(l.jobs), dim3(256), 0, stream, a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+}  // namespace
+
+hipError_t launch_full_bwd(const FullCall& f, const FullPlan& dq, const FullPlan& dkv, float* D, hipStream_t stream) {
+    const int32_t w = f.d > f.dv ? f.d : f.dv;
+#define KMIP_FULL_BWD(W) \
+    if (w == W) return f.fp16 ? launch_bwd<Fp16, W>(f, dq, dkv, D, stream) : launch_bwd<Bf16, W>(f, dq, dkv, D, stream);
+    KMIP_FULL_BWD(16)
+    KMIP_FULL_BWD(32)
+    KMIP_FULL_BWD(64)
+    KMIP_FULL_BWD(128)
+#undef KMIP_FULL_BWD
+    return hipErrorInvalidValue;
+}
+
+}  // namespace kmip

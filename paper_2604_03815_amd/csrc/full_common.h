@@ -178,6 +178,7 @@ struct TileLoad {
 };
 
 // ---- jobs (full_plan.h) ----
+
 // The sequence a job belongs to (uniform over the workgroup).
 __device__ __forceinline__ int seq_of_job(const FullSeqs& s, int32_t job, int lane) {
     int n = 0;
@@ -185,6 +186,98 @@ __device__ __forceinline__ int seq_of_job(const FullSeqs& s, int32_t job, int la
     for (int i = 0; i < kFullSeqs; i += 64)
         n += __popcll(__ballot(i + lane < s.count && s.job0[i + lane] <= job));
     return n - 1;
+}
+
+// A job of a row tile: ROWS rows of one key head's list, and the run of keys
+// it takes (all of them where split is 0).
+struct RowJob {
+    int32_t q_lo, q_len, k_lo, k_len, kv_head, tile, run, runs;
+};
+
+template <int ROWS>
+__device__ __forceinline__ RowJob row_job(const FullSeqs& seqs, int32_t Hk, int32_t rep, int32_t causal, int32_t split,
+                                          int32_t job, int lane) {
+    const int s = __builtin_amdgcn_readfirstlane(seq_of_job(seqs, job, lane));
+    RowJob j;
+    j.q_lo = seqs.q_lo[s];
+    j.q_len = seqs.q_len[s];
+    j.k_lo = seqs.k_lo[s];
+    j.k_len = seqs.k_len[s];
+    j.runs = split > 0 && j.k_len > split ? (j.k_len - 1) / split + 1 : 1;
+    const int32_t tiles = (int32_t)(((int64_t)j.q_len * rep + ROWS - 1) / ROWS);
+    // key heads first: with 8 of them (or a divisor) workgroups of one XCD,
+    // which come round robin, share a head's keys in its L2
+    int32_t rest = job - seqs.job0[s];
+    j.kv_head = rest % Hk;
+    rest /= Hk;
+    j.run = rest % j.runs;
+    // causal: the tiles with the most keys first
+    j.tile = rest / j.runs;
+    if (causal) j.tile = tiles - 1 - j.tile;
+    return j;
+}
+
+// The right operand of 32 columns from a strided tensor: this lane's row
+// (16-byte aligned, `cols` values), zeros behind its width.
+template <int D>
+__device__ __forceinline__ void load_columns(s16x8 (&x)[D / 16], const char* row, int32_t cols, int lane) {
+#pragma unroll
+    for (int t = 0; t < D / 16; ++t) {
+        const int col = 16 * t + 8 * (lane >> 5);
+        if (col < cols)
+            x[t] = *reinterpret_cast<const s16x8*>(row + 2 * col);
+        else
+            x[t] = s16x8{};
+    }
+}
+
+__device__ __forceinline__ void clear(f32x16& x) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) x[r] = 0.0f;
+}
+
+// Registers 8 i .. 8 i + 7, rounded: the right operand for 16 streamed rows.
+template <typename T>
+__device__ __forceinline__ s16x8 round8(const f32x16& x, int i) {
+    s16x8 p;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) p[e] = T::round(x[8 * i + e]);
+    return p;
+}
+
+// Stores column tile t of a transposed result (this lane's row at `row`),
+// times f.
+template <typename T>
+__device__ __forceinline__ void store_piece(uint16_t* row, const f32x16& x, int t, float f, int32_t cols, int lane) {
+#pragma unroll
+    for (int r = 0; r < 16; r += 4) {
+        const int col = 32 * t + 2 * r + 4 * (lane >> 5);
+        if (col < cols) {
+            s16x4 y;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] = T::round(x[r + e] * f);
+            *reinterpret_cast<s16x4*>(row + col) = y;
+        }
+    }
+}
+
+// A wave's transposed result of 32 rows to LDS at so, rows of D floats, their
+// groups of four turned by the row (so that the rows meet different banks).
+template <int D>
+__device__ __forceinline__ void put_piece(float* so, const f32x16& x, int t, float f, int lane) {
+    const int rw = lane & 31;
+#pragma unroll
+    for (int r = 0; r < 16; r += 4) {
+        const int g = 8 * t + (r >> 1) + (lane >> 5);
+        if (4 * g < D)
+            *reinterpret_cast<f32x4*>(so + rw * D + 4 * ((g ^ rw) & (D / 4 - 1))) =
+                f32x4{x[r] * f, x[r + 1] * f, x[r + 2] * f, x[r + 3] * f};
+    }
+}
+
+template <int D>
+__device__ __forceinline__ f32x4 get_piece(const float* so, int row, int g) {
+    return *reinterpret_cast<const f32x4*>(so + row * D + 4 * ((g ^ row) & (D / 4 - 1)));
 }
 
 }  // namespace kmip

@@ -38,32 +38,6 @@ struct FwdArgs {
     FullSeqs s;
 };
 
-struct Job {
-    int32_t q_lo, q_len, k_lo, k_len, kv_head, tile, run, runs;
-};
-
-template <int ROWS>
-__device__ __forceinline__ Job find_job(const FwdArgs& a, int32_t job, int lane) {
-    const int s = __builtin_amdgcn_readfirstlane(seq_of_job(a.s, job, lane));
-    Job j;
-    j.q_lo = a.s.q_lo[s];
-    j.q_len = a.s.q_len[s];
-    j.k_lo = a.s.k_lo[s];
-    j.k_len = a.s.k_len[s];
-    j.runs = a.split > 0 && j.k_len > a.split ? (j.k_len + a.split - 1) / a.split : 1;
-    const int32_t tiles = (int32_t)(((int64_t)j.q_len * a.rep + ROWS - 1) / ROWS);
-    // key heads first: with 8 of them (or a divisor) workgroups of one XCD,
-    // which come round robin, share a head's keys in its L2
-    int32_t rest = job - a.s.job0[s];
-    j.kv_head = rest % a.Hk;
-    rest /= a.Hk;
-    j.run = rest % j.runs;
-    // causal: the tiles with the most keys first
-    j.tile = rest / j.runs;
-    if (a.causal) j.tile = tiles - 1 - j.tile;
-    return j;
-}
-
 // A wave's running state: 32 columns of rows, two lanes a column.
 template <typename T, int D>
 struct FwdWave {
@@ -80,8 +54,7 @@ struct FwdWave {
         f32x16 s[NB];
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
-#pragma unroll
-            for (int r = 0; r < 16; ++r) s[b][r] = 0.0f;
+            clear(s[b]);
 #pragma unroll
             for (int t = 0; t < D / 16; ++t) s[b] = T::mfma(lds_row16((ka ^ (32 * t)) + b * 64 * D), q[t], s[b]);
         }
@@ -125,9 +98,8 @@ struct FwdWave {
             l += sum;
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                s16x8 p;   // rounded to the inputs' type: half a step of each weight, the operand of the product
-#pragma unroll
-                for (int e = 0; e < 8; ++e) p[e] = T::round(s[b][8 * i + e]);
+                // rounded to the inputs' type, the operand of the product: half a step of each weight
+                const s16x8 p = round8<T>(s[b], i);
 #pragma unroll
                 for (int t = 0; t < kT; ++t) {
                     const uint32_t at = (32 * b + 16 * i) * 2 * D;
@@ -148,7 +120,7 @@ __global__ __launch_bounds__(256, ROWS == 128 ? 2 : 1) void full_fwd_kernel(cons
     static_assert(ROWS == 128 || kOwn * 4 * kBytes >= 32 * D * 4 * kWaves, "room for the join");
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const Job j = find_job<ROWS>(a, blockIdx.x, lane);
+    const RowJob j = row_job<ROWS>(a.s, a.Hk, a.rep, a.causal, a.split, blockIdx.x, lane);
     const int32_t nrows = j.q_len * a.rep;
     const int32_t row0 = j.tile * ROWS + (ROWS == 128 ? 32 * wave : 0);
     const int32_t off = j.k_len - j.q_len;
@@ -161,21 +133,9 @@ __global__ __launch_bounds__(256, ROWS == 128 ? 2 : 1) void full_fwd_kernel(cons
     const int32_t token = min(row, nrows - 1) / a.rep, head = j.kv_head * a.rep + min(row, nrows - 1) % a.rep;
 
     FwdWave<T, D> w;
-    {
-        const char* qp = a.q + (j.q_lo + (int64_t)token) * a.q_row + head * a.q_head;
+    load_columns<D>(w.q, a.q + (j.q_lo + (int64_t)token) * a.q_row + head * a.q_head, a.d, lane);
 #pragma unroll
-        for (int t = 0; t < D / 16; ++t) {
-            const int col = 16 * t + 8 * (lane >> 5);
-            if (col < a.d)
-                w.q[t] = *reinterpret_cast<const s16x8*>(qp + 2 * col);
-            else
-                w.q[t] = s16x8{};
-        }
-    }
-#pragma unroll
-    for (int t = 0; t < kT; ++t)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) w.o[t][r] = 0.0f;
+    for (int t = 0; t < kT; ++t) clear(w.o[t]);
     w.m = -INFINITY;
     w.l = 0.0f;
     w.lim = sees(row);
@@ -253,17 +213,7 @@ __global__ __launch_bounds__(256, ROWS == 128 ? 2 : 1) void full_fwd_kernel(cons
         const int64_t at = (j.q_lo + (int64_t)token) * a.H + head;
         const float f = l > 0.0f ? 1.0f / l : 0.0f;
 #pragma unroll
-        for (int t = 0; t < kT; ++t)
-#pragma unroll
-            for (int r = 0; r < 16; r += 4) {
-                const int col = 32 * t + 8 * (r >> 2) + 4 * h;
-                if (col < a.dv) {
-                    s16x4 x;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) x[e] = T::round(w.o[t][r + e] * f);
-                    *reinterpret_cast<s16x4*>(a.out + at * a.dv + col) = x;
-                }
-            }
+        for (int t = 0; t < kT; ++t) store_piece<T>(a.out + at * a.dv, w.o[t], t, f, a.dv, lane);
         if (h == 0) a.lse[at] = l > 0.0f ? (mc + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
     } else {
         // The four waves' sums of the same rows: to a common reference, added in
@@ -280,16 +230,8 @@ __global__ __launch_bounds__(256, ROWS == 128 ? 2 : 1) void full_fwd_kernel(cons
 #pragma unroll
         for (int i = 0; i < kWaves; ++i) top = fmaxf(top, sm[i][rw]);
         const float f = mc == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mc - top);
-        // rows of D + 4 values would not fit; the columns' groups of four are turned by the row instead
 #pragma unroll
-        for (int t = 0; t < kT; ++t)
-#pragma unroll
-            for (int r = 0; r < 16; r += 4) {
-                const int g = 8 * t + 2 * (r >> 2) + h;
-                if (4 * g < D)
-                    *reinterpret_cast<f32x4*>(so + (wave * 32 + rw) * D + 4 * ((g ^ rw) & (D / 4 - 1))) =
-                        f32x4{w.o[t][r] * f, w.o[t][r + 1] * f, w.o[t][r + 2] * f, w.o[t][r + 3] * f};
-            }
+        for (int t = 0; t < kT; ++t) put_piece<D>(so + wave * 32 * D, w.o[t], t, f, lane);
         wait_and_sync();
         for (int i = threadIdx.x; i < 32 * (D / 4); i += 256) {
             const int rr = i / (D / 4), g = i % (D / 4);
@@ -299,7 +241,7 @@ __global__ __launch_bounds__(256, ROWS == 128 ? 2 : 1) void full_fwd_kernel(cons
             float mm = -INFINITY, ll = 0.0f;
 #pragma unroll
             for (int u = 0; u < kWaves; ++u) {
-                x += *reinterpret_cast<const f32x4*>(so + (u * 32 + rr) * D + 4 * ((g ^ rr) & (D / 4 - 1)));
+                x += get_piece<D>(so + u * 32 * D, rr, g);
                 mm = fmaxf(mm, sm[u][rr]);
             }
 #pragma unroll
@@ -333,7 +275,7 @@ __global__ __launch_bounds__(256) void full_join_kernel(const FwdArgs a) {
     __shared__ f32x4 part[256];
     __shared__ float wm[4], wl[4];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const Job j = find_job<ROWS>(a, blockIdx.x, lane);
+    const RowJob j = row_job<ROWS>(a.s, a.Hk, a.rep, a.causal, a.split, blockIdx.x, lane);
     if (j.runs == 1 || j.run != 0) return;
     const int32_t row = j.tile * ROWS + blockIdx.y;
     if (row >= j.q_len * a.rep) return;

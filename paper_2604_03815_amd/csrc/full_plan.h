@@ -17,7 +17,7 @@ namespace kmip {
 constexpr int kFullSeqs = 128;
 
 struct FullSeqs {
-    int32_t q_lo[kFullSeqs], q_len[kFullSeqs], k_lo[kFullSeqs], k_len[kFullSeqs], job0[kFullSeqs];
+    int32_t q_lo[kFullSeqs], q_len[kFullSeqs], k_lo[kFullSeqs], k_len[kFullSeqs], k_slot[kFullSeqs], job0[kFullSeqs];
     int32_t count;
 };
 
@@ -47,6 +47,9 @@ struct FullPlan {
     std::vector<FullLaunch> launches;
 };
 
+// dQ first (plan dq; it also writes D [Nq, H]), then dK and dV (plan dkv, rows: keys
+// of a job).
+hipError_t launch_full_bwd(const FullCall& f, const FullPlan& dq, const FullPlan& dkv, float* D, hipStream_t stream);
 hipError_t launch_full_fwd(const FullCall& f, const FullPlan& p, float* part_o, float* part_ml, hipStream_t stream);
 
 }  // namespace kmip

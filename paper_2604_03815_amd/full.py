@@ -158,3 +158,63 @@ def full_fwd(q, k_, v, scale: float, graph_offsets: Optional[Sequence[int]] = No
                                 int(bool(causal)), _ptr(out), _ptr(lse), _ptr(buf), 0 if buf is None else buf.numel(),
                                 stream))
     return out, lse
+
+
+def full_bwd_workspace_size(Nq: int, Nk: int, H: int, Hk: int, d: int, dv: int, graph_offsets=None, key_offsets=None,
+                            key_lengths=None) -> int:
+    keep, ptrs, G = _sequences(graph_offsets, key_offsets, key_lengths)
+    return int(load().kmip_full_bwd_workspace_size(*ptrs, G, Nq, Nk, H, Hk, d, dv))
+
+
+def full_bwd(q, k_, v, dout, out, lse, scale: float, graph_offsets: Optional[Sequence[int]] = None, key_offsets=None,
+             key_lengths=None, causal: bool = False, dq=None, dk=None, dv=None, workspace=None):
+    """Gradients of full softmax attention: returns (dQ, dK, dV) of the inputs' type."""
+    Nq, Nk, H, Hk, d, wv = _sizes(q, k_, v)
+    sizes, strides, code = _inputs(q, k_, v, (dout, "dOut", (Nq, H, wv)))
+    _output(out, "out", q.dtype, (Nq, H, wv), None)
+    _output(lse, "lse", torch.float32, (Nq, H), None)
+    shapes = ((dq, "dQ", (Nq, H, d)), (dk, "dK", (Nk, Hk, d)), (dv, "dV", (Nk, Hk, wv)))
+    given = [(t, n) for t, n, shape in shapes if t is not None and _output(t, n, q.dtype, shape, None) is not None]
+    keep, ptrs, G = _sequences(graph_offsets, key_offsets, key_lengths)
+    dev = _check_devices((q, "Q"), (k_, "K"), (v, "V"), (dout, "dOut"), (out, "out"), (lse, "lse"), *given)
+    dq, dk, dv = (_output(t, n, q.dtype, shape, dev) for t, n, shape in shapes)
+    lib = load()
+    buf = _scratch(workspace, lib.kmip_full_bwd_workspace_size(*ptrs, G, *sizes), dev)
+    with _on_device(dev) as stream:
+        check(lib.kmip_full_bwd(_ptr(q), _ptr(k_), _ptr(v), _ptr(dout), _ptr(out), _ptr(lse), code, strides, *ptrs, G,
+                                *sizes, float(scale), int(bool(causal)), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(buf),
+                                0 if buf is None else buf.numel(), stream))
+    return dq, dk, dv
+
+
+def full_attention(q, k_, v, scale: float, graph_offsets: Optional[Sequence[int]] = None, key_offsets=None,
+                   key_lengths=None, causal: bool = False, workspace=None):
+    """Differentiable full softmax attention: returns out [Nq, H, dv] of the inputs' type.
+
+    The forward is ``full_fwd``; autograd's backward calls ``full_bwd`` with
+    the saved out and lse.  Once differentiable.
+    """
+    where = dict(graph_offsets=graph_offsets, key_offsets=key_offsets, key_lengths=key_lengths, causal=causal)
+    return _full_function().apply(q, k_, v, scale, where, workspace)
+
+
+@functools.lru_cache(maxsize=None)
+def _full_function():
+    class _Full(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, q, k_, v, scale, where, workspace):
+            out, lse = full_fwd(q, k_, v, scale, workspace=workspace, **where)
+            ctx.save_for_backward(q, k_, v, out, lse)
+            ctx.args = scale, where, workspace
+            return out
+
+        @staticmethod
+        @torch.autograd.function.once_differentiable
+        def backward(ctx, dout):
+            q, k_, v, out, lse = ctx.saved_tensors
+            scale, where, workspace = ctx.args
+            if dout.stride(-1) != 1 or any(s % 8 for s in dout.stride()[:2]) or dout.data_ptr() % 16:
+                dout = dout.contiguous()
+            return (*full_bwd(q, k_, v, dout, out, lse, scale, workspace=workspace, **where), None, None, None)
+
+    return _Full

@@ -63,3 +63,21 @@ def test_forward(i):
     check("lse", lse, want["lse"])
     again = kmip.full_fwd(q, k, v, scale, causal=causal, **where)
     assert torch.equal(out, again[0]) and torch.equal(lse, again[1])
+
+
+@pytest.mark.parametrize("i", range(len(CASES)))
+def test_backward(i):
+    dtype, H, Hk, d, dv, lens, causal = CASES[i]
+    ql, kl = zip(*lens)
+    q, k, v, dout = make(100 + i, sum(ql), sum(kl), H, Hk, d, dv, dtype)
+    scale = 1.0 / math.sqrt(d)
+    where = dict(graph_offsets=sums(ql), key_offsets=sums(kl))
+    out, lse = kmip.full_fwd(q, k, v, scale, causal=causal, **where)
+    got = kmip.full_bwd(q, k, v, dout, out, lse, scale, causal=causal, **where)
+    want = full64(q, k, v, scale, sequences(len(q), len(k), **where), causal, dout)
+    for name, x in zip(("dq", "dk", "dv"), got):
+        assert x.dtype == dtype
+        check(name, x, want[name])
+    again = kmip.full_bwd(q, k, v, dout, out, lse, scale, causal=causal, **where)
+    for x, y in zip(got, again):
+        assert torch.equal(x, y)
