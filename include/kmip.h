@@ -378,6 +378,28 @@ kmip_status_t kmip_full_bwd(const void* Q, const void* K, const void* V, const v
                             int32_t H, int32_t Hk, int32_t d, int32_t dv, float scale, int32_t causal, void* dQ, void* dK,
                             void* dV, void* workspace, size_t workspace_bytes, void* stream);
 
+/*
+ * Rotary positions on the rows of one or two tensors (queries and keys) in one
+ * launch.  Pair i of a row's first `rot` dimensions (interleaved != 0:
+ * dimensions 2i and 2i + 1; else i and i + rot / 2) is turned by
+ * t = position * freqs[i] radians and scaled by `magnitude`:
+ *   (a, b) -> magnitude (a cos t - b sin t, b cos t + a sin t);
+ * dimensions from rot on are passed on.  inverse != 0 turns by -t: with the same
+ * magnitude the gradient of the forward call.
+ *  - X, Y [N, H, d], X2, Y2 [N, H2, d] (H2 = 0: none) of types dtype_in and dtype_out
+ *    (each KMIP_BF16, KMIP_FP16 or KMIP_FP32); d even, at most 256.
+ *  - strides: HOST int64 [8], values between the rows and the heads of X, Y, X2, Y2, or
+ *    NULL: contiguous.  Y may be X (same type and strides); other overlaps are not allowed.
+ *  - positions: device int32 [N], any values, or NULL: row i is at position i.
+ *  - freqs: HOST float64 [rot / 2], read before the call returns (they travel in the
+ *    kernel's arguments; the call can be captured into a HIP graph).
+ *    The angle of position p is exact to |p| 2^-53 of the angle a position plus 2^-31 radians.
+ */
+kmip_status_t kmip_rotary(const void* X, void* Y, int32_t H, const void* X2, void* Y2, int32_t H2, int32_t dtype_in,
+                          int32_t dtype_out, const int64_t* strides, const int32_t* positions, const double* freqs,
+                          int64_t N, int32_t d, int32_t rot, int32_t interleaved, float magnitude, int32_t inverse,
+                          void* stream);
+
 /* Static description of a status code. */
 const char* kmip_status_string(kmip_status_t status);
 

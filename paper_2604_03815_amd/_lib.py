@@ -28,7 +28,7 @@ EXPORTS = (
     "kmip_fwd", "kmip_attend_ex", "kmip_fwd_ex", "kmip_fwd_ex_with_events", "kmip_bwd_workspace_size", "kmip_bwd",
     "kmip_bwd_ex_workspace_size", "kmip_bwd_ex", "kmip_fwd_noalloc", "kmip_topk_prefilter_workspace_size",
     "kmip_topk_prefilter", "kmip_full_fwd_workspace_size", "kmip_full_fwd",
-    "kmip_full_bwd_workspace_size", "kmip_full_bwd", "kmip_status_string", "kmip_last_error",
+    "kmip_full_bwd_workspace_size", "kmip_full_bwd", "kmip_rotary", "kmip_status_string", "kmip_last_error",
 )
 
 # kmip_dtype_t
@@ -86,10 +86,11 @@ def load(path: str = LIB_PATH):
     lib.kmip_full_bwd_workspace_size.argtypes = offsets
     lib.kmip_full_bwd_workspace_size.restype = sz
     lib.kmip_full_bwd.argtypes = [P, P, P, P, P, P, i32, P, *offsets, f32, i32, P, P, P, P, sz, P]
+    lib.kmip_rotary.argtypes = [P, P, i32, P, P, i32, i32, i32, P, P, P, i64, i32, i32, i32, f32, i32, P]
     lib.kmip_full_fwd.argtypes = [P, P, P, i32, P, *offsets, f32, i32, P, P, P, sz, P]
     for f in ("kmip_topk", "kmip_topk_with_events", "kmip_attend", "kmip_fwd", "kmip_bwd",
               "kmip_fwd_noalloc", "kmip_attend_ex", "kmip_fwd_ex", "kmip_fwd_ex_with_events", "kmip_bwd_ex",
-              "kmip_topk_prefilter", "kmip_full_fwd", "kmip_full_bwd"):
+              "kmip_topk_prefilter", "kmip_full_fwd", "kmip_full_bwd", "kmip_rotary"):
         getattr(lib, f).restype = ctypes.c_int
     lib.kmip_status_string.argtypes = [ctypes.c_int]
     lib.kmip_status_string.restype = ctypes.c_char_p

@@ -1,0 +1,267 @@
+// Rotary positions (gfx950): each pair (a, b) of a row's first `rot` dimensions
+// is turned by t = position * frequency and scaled by m,
+//   (a, b) -> m (a cos t - b sin t, b cos t + a sin t);
+// a pair is two neighbours (interleaved) or dimensions i and i + rot / 2.
+// The gradient of a turn is the turn back, so one kernel serves both.
+//
+// Angles: the frequency in turns a position is held as a 64-bit fraction, so
+// position * frequency modulo one turn is one wrapping integer product, exact
+// but for the fraction's own rounding (position * 2^-65 turns): far positions
+// lose nothing.  Its top two bits (rounded) pick the quadrant; the rest, at most
+// pi/4, goes through the Taylor sums of sine and cosine (to x^9 and x^10:
+// remainders below 2e-9).  All in float32; the row's values are rounded once.
+//
+// A thread takes P pairs of one token for a group of heads, so that an angle is
+// formed once for many heads.  Bound by memory: a row is read once and written
+// once, 16 bytes a lane where the sizes allow.
+#include <cmath>
+#include <cstring>
+
+#include "kmip_device.h"
+#include "kmip_internal.h"
+
+namespace kmip {
+namespace {
+
+constexpr int kMostPairs = 128;
+
+struct Side {
+    const char* x;
+    char* y;
+    int64_t x_row, x_head, y_row, y_head;   // bytes
+};
+
+struct RotaryArgs {
+    Side s[2];
+    const int32_t* positions;
+    uint32_t threads;                 // N * units
+    int32_t units, rot_units;         // threads a token and head group, those with pairs
+    int32_t heads, first_heads, group;
+    int32_t rot;
+    float cos_scale, sin_scale;
+    uint64_t turns[kMostPairs];
+};
+
+struct Half16 {   // float16
+    typedef uint16_t word;
+    static __device__ __forceinline__ float widen(uint16_t x) { return (float)__builtin_bit_cast(_Float16, x); }
+    static __device__ __forceinline__ uint16_t round(float x) { return __builtin_bit_cast(uint16_t, (_Float16)x); }
+};
+struct Brain16 {   // bfloat16
+    typedef uint16_t word;
+    static __device__ __forceinline__ float widen(uint16_t x) { return bf16_bits_to_f32(x); }
+    static __device__ __forceinline__ uint16_t round(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
+};
+struct Single {
+    typedef float word;
+    static __device__ __forceinline__ float widen(float x) { return x; }
+    static __device__ __forceinline__ float round(float x) { return x; }
+};
+
+// P values of type T at p, aligned to their size or 16 bytes.
+template <typename T, int P>
+struct alignas(sizeof(typename T::word) * P < 16 ? sizeof(typename T::word) * P : 16) Pack {
+    typename T::word v[P];
+};
+
+template <typename T, int P>
+__device__ __forceinline__ void load(float (&x)[P], const char* p) {
+    const Pack<T, P> w = *reinterpret_cast<const Pack<T, P>*>(p);
+#pragma unroll
+    for (int e = 0; e < P; ++e) x[e] = T::widen(w.v[e]);
+}
+
+template <typename T, int P>
+__device__ __forceinline__ void store(char* p, const float (&x)[P]) {
+    Pack<T, P> w;
+#pragma unroll
+    for (int e = 0; e < P; ++e) w.v[e] = T::round(x[e]);
+    *reinterpret_cast<Pack<T, P>*>(p) = w;
+}
+
+// sin and cos of phase / 2^32 turns.
+__device__ __forceinline__ void sin_cos(uint32_t phase, float* s, float* c) {
+    const uint32_t quarter = (phase + 0x20000000u) >> 30;
+    const float x = (float)(int32_t)(phase - (quarter << 30)) * 1.4629180792671596e-9f;   // 2 pi / 2^32
+    const float z = x * x;
+    const float sn = x + x * z * (-1.0f / 6 + z * (1.0f / 120 + z * (-1.0f / 5040 + z * (1.0f / 362880))));
+    const float cs = 1.0f + z * (-0.5f + z * (1.0f / 24 + z * (-1.0f / 720 + z * (1.0f / 40320 - z * (1.0f / 3628800)))));
+    const float u = (quarter & 1) ? cs : sn, w = (quarter & 1) ? sn : cs;
+    *s = (quarter & 2) ? -u : u;
+    *c = ((quarter + 1) & 2) ? -w : w;
+}
+
+template <typename TI, typename TO, int P, bool INTER>
+__global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs a) {
+    constexpr int kIn = sizeof(typename TI::word), kOut = sizeof(typename TO::word);
+    const uint32_t id = blockIdx.x * 256u + threadIdx.x;
+    if (id >= a.threads) return;
+    const uint32_t token = id / (uint32_t)a.units;
+    const int unit = (int)(id - token * (uint32_t)a.units);
+    const bool turned = unit < a.rot_units;
+    // first and second run of P values in the row
+    int one = 2 * P * unit, two = one + P;
+    float c[P], s[P];
+    if (turned) {
+        if (!INTER) one = P * unit, two = one + a.rot / 2;
+        const uint64_t pos = (uint64_t)(int64_t)(a.positions != nullptr ? a.positions[token] : (int32_t)token);
+#pragma unroll
+        for (int e = 0; e < P; ++e) {
+            sin_cos((uint32_t)((pos * a.turns[P * unit + e]) >> 32), &s[e], &c[e]);
+            c[e] *= a.cos_scale;
+            s[e] *= a.sin_scale;
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < P; ++e) c[e] = 1.0f, s[e] = 0.0f;
+    }
+    const int h0 = blockIdx.y * a.group, h1 = min(h0 + a.group, a.heads);
+#pragma unroll 4
+    for (int h = h0; h < h1; ++h) {
+        const bool second = h >= a.first_heads;
+        const Side& t = a.s[second];
+        const int hh = second ? h - a.first_heads : h;
+        const char* x = t.x + (int64_t)token * t.x_row + hh * t.x_head;
+        char* y = t.y + (int64_t)token * t.y_row + hh * t.y_head;
+        float u[P], v[P], p[P], q[P];
+        load<TI, P>(u, x + one * kIn);
+        load<TI, P>(v, x + two * kIn);
+        if (!turned) {
+            store<TO, P>(y + one * kOut, u);
+            store<TO, P>(y + two * kOut, v);
+            continue;
+        }
+        if constexpr (INTER) {   // u, v: 2 P neighbours
+            float w[2 * P];
+#pragma unroll
+            for (int e = 0; e < P; ++e) w[e] = u[e], w[P + e] = v[e];
+#pragma unroll
+            for (int e = 0; e < P; ++e) {
+                const float f = w[2 * e] * c[e] - w[2 * e + 1] * s[e], g = w[2 * e + 1] * c[e] + w[2 * e] * s[e];
+                w[2 * e] = f;
+                w[2 * e + 1] = g;
+            }
+#pragma unroll
+            for (int e = 0; e < P; ++e) p[e] = w[e], q[e] = w[P + e];
+        } else {
+#pragma unroll
+            for (int e = 0; e < P; ++e) {
+                p[e] = u[e] * c[e] - v[e] * s[e];
+                q[e] = v[e] * c[e] + u[e] * s[e];
+            }
+        }
+        store<TO, P>(y + one * kOut, p);
+        store<TO, P>(y + two * kOut, q);
+    }
+}
+
+int32_t size_of(int32_t dtype) { return dtype == KMIP_FP32 ? 4 : 2; }
+
+kmip_status_t ok() { return record_error(KMIP_OK, "%s", ""); }
+
+template <typename TI, typename TO>
+void launch_types(const RotaryArgs& a, int pairs, bool inter, dim3 grid, hipStream_t stream) {
+#define KMIP_ROTARY(P)                                                                                       \
+    if (pairs == P) {                                                                                        \
+        if (inter)                                                                                           \
+            hipLaunchKernelGGL((rotary_kernel<TI, TO, P, true>), grid, dim3(256), 0, stream, a);             \
+        else                                                                                                 \
+            hipLaunchKernelGGL((rotary_kernel<TI, TO, P, false>), grid, dim3(256), 0, stream, a);            \
+    }
+    KMIP_ROTARY(8)
+    KMIP_ROTARY(4)
+    KMIP_ROTARY(1)
+#undef KMIP_ROTARY
+}
+
+template <typename TI>
+void launch_out(const RotaryArgs& a, int32_t out, int pairs, bool inter, dim3 grid, hipStream_t stream) {
+    if (out == KMIP_BF16) launch_types<TI, Brain16>(a, pairs, inter, grid, stream);
+    if (out == KMIP_FP16) launch_types<TI, Half16>(a, pairs, inter, grid, stream);
+    if (out == KMIP_FP32) launch_types<TI, Single>(a, pairs, inter, grid, stream);
+}
+
+}  // namespace
+}  // namespace kmip
+
+extern "C" kmip_status_t kmip_rotary(const void* X, void* Y, int32_t H, const void* X2, void* Y2, int32_t H2,
+                                     int32_t dtype_in, int32_t dtype_out, const int64_t* strides, const int32_t* positions,
+                                     const double* freqs, int64_t N, int32_t d, int32_t rot, int32_t interleaved,
+                                     float magnitude, int32_t inverse, void* stream) {
+    using namespace kmip;
+    if (N < 0 || N >= (int64_t(1) << 31)) return record_error(KMIP_ERR_INVALID_ARG, "N=%lld out of range", (long long)N);
+    if (H < 1 || H2 < 0 || (int64_t)H + H2 >= (1 << 20)) return record_error(KMIP_ERR_INVALID_ARG, "H=%d, H2=%d", H, H2);
+    if (d < 2 || d > 2 * kMostPairs || d % 2 != 0) return record_error(KMIP_ERR_UNSUPPORTED, "d=%d must be even, 2 .. %d", d, 2 * kMostPairs);
+    if (rot < 2 || rot > d || rot % 2 != 0) return record_error(KMIP_ERR_INVALID_ARG, "rot=%d must be even, 2 .. d", rot);
+    if (dtype_in < KMIP_BF16 || dtype_in > KMIP_FP32 || dtype_out < KMIP_BF16 || dtype_out > KMIP_FP32)
+        return record_error(KMIP_ERR_UNSUPPORTED, "dtypes %d, %d", dtype_in, dtype_out);
+    if (freqs == nullptr) return record_error(KMIP_ERR_INVALID_ARG, "null freqs");
+    uint32_t bits;
+    std::memcpy(&bits, &magnitude, sizeof(bits));
+    if ((bits & 0x7F800000u) == 0x7F800000u) return record_error(KMIP_ERR_INVALID_ARG, "magnitude must be finite");
+    RotaryArgs a{};
+    for (int32_t i = 0; i < rot / 2; ++i) {
+        uint64_t fb;
+        std::memcpy(&fb, &freqs[i], sizeof(fb));
+        if (((fb >> 52) & 0x7FF) == 0x7FF) return record_error(KMIP_ERR_INVALID_ARG, "freqs[%d] is not finite", i);
+        // the fraction of a turn (round to nearest; one whole turn wraps to 0)
+        const long double turns = (long double)freqs[i] / 6.283185307179586476925286766559005768L;
+        const long double part = turns - floorl(turns);
+        a.turns[i] = part >= 1.0L - 0x1p-65L ? 0 : (uint64_t)(part * 0x1p64L + 0.5L);
+    }
+    if (N == 0) return ok();
+    if (!X || !Y || (H2 > 0 && (!X2 || !Y2))) return record_error(KMIP_ERR_INVALID_ARG, "null buffer passed to kmip_rotary");
+    const int32_t si = size_of(dtype_in), so = size_of(dtype_out);
+    const int64_t packed[8] = {(int64_t)H * d, d, (int64_t)H * d, d, (int64_t)H2 * d, d, (int64_t)H2 * d, d};
+    const int64_t* st = strides != nullptr ? strides : packed;
+    // the widest runs of pairs that sizes, strides and pointers allow
+    int pairs = 8;
+    auto fits = [&](int p) {
+        if (rot / 2 % p != 0 || (d - rot) % (2 * p) != 0) return false;
+        const int32_t bi = p * si < 16 ? p * si : 16, bo = p * so < 16 ? p * so : 16;
+        for (int t = 0; t < (H2 > 0 ? 2 : 1); ++t) {
+            const void *x = t ? X2 : X, *y = t ? Y2 : Y;
+            if (reinterpret_cast<uintptr_t>(x) % bi != 0 || reinterpret_cast<uintptr_t>(y) % bo != 0) return false;
+            for (int i = 0; i < 2; ++i)
+                if (st[4 * t + i] * si % bi != 0 || st[4 * t + 2 + i] * so % bo != 0) return false;
+        }
+        return true;
+    };
+    if (!fits(8)) pairs = fits(4) ? 4 : 1;
+    for (int t = 0; t < (H2 > 0 ? 2 : 1); ++t) {
+        const void *x = t ? X2 : X, *y = t ? Y2 : Y;
+        if (reinterpret_cast<uintptr_t>(x) % si != 0 || reinterpret_cast<uintptr_t>(y) % so != 0)
+            return record_error(KMIP_ERR_INVALID_ARG, "buffers must be aligned to their type");
+        for (int i = 0; i < 4; ++i)
+            if (st[4 * t + i] < 0) return record_error(KMIP_ERR_INVALID_ARG, "negative stride");
+        if (x == y && (si != so || st[4 * t] != st[4 * t + 2] || st[4 * t + 1] != st[4 * t + 3]))
+            return record_error(KMIP_ERR_INVALID_ARG, "in place needs one type and the same strides");
+        a.s[t] = Side{static_cast<const char*>(t ? X2 : X), static_cast<char*>(t ? Y2 : Y), st[4 * t] * si,
+                      st[4 * t + 1] * si, st[4 * t + 2] * so, st[4 * t + 3] * so};
+    }
+    a.positions = positions;
+    a.units = d / (2 * pairs);
+    a.rot_units = rot / 2 / pairs;
+    const int64_t threads = N * a.units;
+    if (threads >= (int64_t(1) << 32) - 256) return record_error(KMIP_ERR_INVALID_ARG, "N * d / %d >= 2^32", 2 * pairs);
+    a.threads = (uint32_t)threads;
+    a.heads = H + H2;
+    a.first_heads = H;
+    // Heads a thread takes: as many as leave 2^18 threads (16 waves a CU)
+    const int64_t groups = (int64_t(1) << 18) / threads + 1;
+    a.group = groups >= a.heads ? 1 : (int32_t)((a.heads + groups - 1) / groups);
+    int32_t ny = (a.heads + a.group - 1) / a.group;
+    if (ny > 65535) a.group = (a.heads + 65534) / 65535, ny = (a.heads + a.group - 1) / a.group;
+    a.rot = rot;
+    a.cos_scale = magnitude;
+    a.sin_scale = inverse ? -magnitude : magnitude;
+    const dim3 grid((unsigned)((threads + 255) / 256), (unsigned)ny);
+    const hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+    const bool inter = interleaved != 0;
+    if (dtype_in == KMIP_BF16) launch_out<Brain16>(a, dtype_out, pairs, inter, grid, s);
+    if (dtype_in == KMIP_FP16) launch_out<Half16>(a, dtype_out, pairs, inter, grid, s);
+    if (dtype_in == KMIP_FP32) launch_out<Single>(a, dtype_out, pairs, inter, grid, s);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return record_error(KMIP_ERR_HIP, "rotary launch: %s", hipGetErrorString(e));
+    return ok();
+}

@@ -1,0 +1,158 @@
+"""Rotary positions on queries and keys: front end of kmip_rotary.
+
+Pair i of a row's first ``rot = 2 len(freqs)`` dimensions (neighbours 2i, 2i + 1
+where ``interleaved``, else dimensions i and i + rot / 2) is turned by
+position * freqs[i] radians and scaled by ``magnitude``; the rest of the row is
+passed on.  The scores of turned queries and keys depend on the difference of their positions.
+"""
+from __future__ import annotations
+
+import ctypes
+import functools
+import math
+from typing import Optional
+
+import numpy as np
+import torch
+
+from ._lib import check, load
+from .full import _DTYPES, _check_devices, _check_view, _on_device, _ptr
+
+
+def rotary_frequencies(rot: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0,
+                       original_length: Optional[int] = None, slow_turns: float = 1.0, fast_turns: float = 32.0):
+    """(freqs float64 [rot / 2] in radians a position, magnitude) for ``rotary``.
+
+    freqs[i] = base^(-2 i / rot); for contexts ``factor`` times longer than the ``original_length`` trained on:
+      "linear"  every frequency divided by the factor;
+      "base"    base times factor^(rot / (rot - 2)): the fastest pair as it was, the slowest divided by the factor;
+      "blend"   pairs that turn less than ``slow_turns`` times in the original length divided by the factor, those that turn more
+                than ``fast_turns`` times as they were, a linear blend in between; magnitude 0.1 log(factor) + 1.
+    """
+    if rot < 2 or rot % 2:
+        raise ValueError("rot must be even and at least 2")
+    if not base > 0 or not factor > 0:
+        raise ValueError("base and factor must be > 0")
+    if scaling == "base" and rot > 2:
+        base = base * factor ** (rot / (rot - 2))
+    freqs = base ** (-2.0 * np.arange(rot // 2, dtype=np.float64) / rot)
+    if scaling in ("none", "base"):
+        return freqs, 1.0
+    if scaling == "linear":
+        return freqs / factor, 1.0
+    if scaling != "blend":
+        raise ValueError('scaling must be "none", "linear", "base" or "blend"')
+    if original_length is None or not 0 <= slow_turns < fast_turns:
+        raise ValueError("blend needs original_length and 0 <= slow_turns < fast_turns")
+    keep = np.clip((original_length * freqs / (2 * math.pi) - slow_turns) / (fast_turns - slow_turns), 0.0, 1.0)
+    return freqs * keep + freqs / factor * (1.0 - keep), 0.1 * math.log(factor) + 1.0
+
+
+def _rows(t, name):
+    if not isinstance(t, torch.Tensor) or t.dim() != 3:
+        raise ValueError(f"{name} must be a tensor [N, heads, d]")
+    if t.dtype not in _DTYPES:
+        raise TypeError(f"{name} must be bfloat16, float16 or float32, got {t.dtype}")
+
+
+def rotary(q, k_=None, positions=None, freqs=None, interleaved: bool = False, magnitude: float = 1.0, inverse: bool = False,
+           dtype=None, q_out=None, k_out=None):
+    """Turns q [N, H, d], and k_ [N, Hk, d] if given, to their positions in one launch: returns q, or (q, k).
+
+    positions: int32 [N] on the device (None: row i is at position i); freqs: host float64 [rot / 2] (``rotary_frequencies``); dtype of the results
+    (default: the inputs'): bfloat16, float16 or float32.  inverse turns back.  q_out, k_out: tensors to write into,
+    q_out=q for in place.  Inputs and outputs may be views whose last dimension is contiguous (outputs must not overlap themselves).
+    Differentiable in q and k_ unless q_out or k_out is given.
+    """
+    if freqs is None:
+        raise ValueError("freqs must be given (see rotary_frequencies)")
+    given = q_out is not None or k_out is not None
+    grad = torch.is_grad_enabled() and any(isinstance(t, torch.Tensor) and t.requires_grad for t in (q, k_))
+    if grad:
+        if given:
+            raise ValueError("q_out and k_out are not differentiable: leave them out, or call under torch.no_grad()")
+        _rows(q, "q")
+        if k_ is not None and not isinstance(k_, torch.Tensor):
+            raise ValueError("k must be a tensor [N, heads, d]")
+        got = _rotary_function().apply(q, k_, positions, freqs, interleaved, magnitude, inverse, dtype)
+        return got[0] if k_ is None else got
+    return _launch(q, k_, positions, freqs, interleaved, magnitude, inverse, dtype, q_out, k_out)
+
+
+def _launch(q, k_, positions, freqs, interleaved, magnitude, inverse, dtype, q_out, k_out):
+    _rows(q, "q")
+    f = np.ascontiguousarray(freqs, dtype=np.float64)
+    if f.ndim != 1:
+        raise ValueError("freqs must be 1-D")
+    N, H, d = q.shape
+    H2 = 0
+    if k_ is not None:
+        _rows(k_, "k")
+        H2 = k_.shape[1]
+    elif k_out is not None:
+        raise ValueError("k_out without k")
+    to = q.dtype if dtype is None else dtype
+    if to not in _DTYPES:
+        raise TypeError(f"dtype must be bfloat16, float16 or float32, got {to}")
+    strides, named = [], [(q, "q")]
+    for t, o, name, heads in ((q, q_out, "q", H), (k_, k_out, "k", H2)):
+        if t is None:
+            strides += [0] * 4
+            continue
+        strides += _check_view(t, name, q.dtype, (N, heads, d))
+        if o is None:
+            strides += [heads * d, d]
+        else:
+            s = _check_view(o, name + "_out", to, (N, heads, d))
+            if min(s[0] if N > 1 else d, s[1] if heads > 1 else d) < d:
+                raise ValueError(f"{name}_out overlaps itself")
+            strides += s
+            named.append((o, name + "_out"))
+        named.append((t, name))
+    if positions is not None:
+        _check_positions(positions, N)
+        named.append((positions, "positions"))
+    dev = _check_devices(*named)
+    q_out = torch.empty((N, H, d), dtype=to, device=dev) if q_out is None else q_out
+    if k_ is not None and k_out is None:
+        k_out = torch.empty((N, H2, d), dtype=to, device=dev)
+    host = (ctypes.c_int64 * 8)(*strides)
+    with _on_device(dev) as stream:
+        check(load().kmip_rotary(_ptr(q), _ptr(q_out), H, _ptr(k_), _ptr(k_out), H2, _DTYPES[q.dtype], _DTYPES[to], host,
+                                 _ptr(positions), ctypes.c_void_p(f.ctypes.data), N, d, 2 * len(f), int(bool(interleaved)),
+                                 float(magnitude), int(bool(inverse)), stream))
+    return q_out if k_ is None else (q_out, k_out)
+
+
+def _check_positions(positions, N):
+    if not isinstance(positions, torch.Tensor):
+        raise TypeError("positions must be a torch tensor")
+    if positions.dtype != torch.int32:
+        raise TypeError(f"positions must be torch.int32, got {positions.dtype}")
+    if tuple(positions.shape) != (N,):
+        raise ValueError(f"positions must have shape {(N,)}, got {tuple(positions.shape)}")
+    if not positions.is_contiguous():
+        raise ValueError("positions must be contiguous")
+
+
+@functools.lru_cache(maxsize=None)
+def _rotary_function():
+    class _Rotary(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, q, k_, positions, freqs, interleaved, magnitude, inverse, dtype):
+            freqs = np.array(freqs, dtype=np.float64)   # (the caller may change its own)
+            got = _launch(q, k_, positions, freqs, interleaved, magnitude, inverse, dtype, None, None)
+            ctx.save_for_backward(*(() if positions is None else (positions,)))
+            ctx.args = freqs, interleaved, magnitude, inverse, q.dtype, k_ is not None
+            return (got,) if k_ is None else got
+
+        @staticmethod
+        @torch.autograd.function.once_differentiable
+        def backward(ctx, dq, dk=None):
+            freqs, interleaved, magnitude, inverse, dtype, both = ctx.args
+            positions = ctx.saved_tensors[0] if ctx.saved_tensors else None
+            dq, dk = (t if t is None or t.shape[-1] < 2 or t.stride(-1) == 1 else t.contiguous() for t in (dq, dk))
+            got = _launch(dq, dk, positions, freqs, interleaved, magnitude, not inverse, dtype, None, None)
+            return (*(got if both else (got, None)), None, None, None, None, None, None)
+
+    return _Rotary
