@@ -84,87 +84,97 @@ bool finite_bits(float x) {   // (the sources are built without NaN tests)
     return (b & 0x7F800000u) != 0x7F800000u;
 }
 
-// Cuts the list of sequences with jobs_of(seq) jobs each into launches, the
-// costliest sequences first (ties in their order), so that the last jobs are
-// short ones.
-template <typename Jobs>
-kmip_status_t cut(std::vector<Seq>& seqs, const Jobs& jobs_of, FullPlan* p) {
+// Cuts the list of sequences, with tiles_of(seq) tiles (of all key heads) of
+// streamed_of(seq) streamed rows each, into launches, the costliest sequences
+// first (ties in their order), so that the last jobs are short ones.
+template <typename Tiles, typename Streamed>
+kmip_status_t cut(std::vector<Seq>& seqs, bool causal, const Tiles& tiles_of, const Streamed& streamed_of, FullPlan* p) {
     auto cost = [](const Seq& s) { return (int64_t)std::max(s.q_len, 1) * std::max(s.k_len, 1); };
     std::stable_sort(seqs.begin(), seqs.end(), [&](const Seq& x, const Seq& y) { return cost(x) > cost(y); });
     p->jobs = 0;
     for (size_t first = 0; first < seqs.size(); first += kmip::kFullSeqs) {
-        FullLaunch l{};
+        p->launches.emplace_back();
+        FullLaunch& l = p->launches.back();
+        std::memset(static_cast<void*>(&l), 0, sizeof(l));
         const size_t n = std::min(seqs.size() - first, (size_t)kmip::kFullSeqs);
-        int64_t jobs = 0;
+        int64_t jobs = 0, tile_jobs = 0;
+        auto put = [](kmip::FullSeqs& q, const Seq& s, int64_t job0) {
+            const int32_t i = q.count++;
+            q.q_lo[i] = s.q_lo, q.q_len[i] = s.q_len, q.k_lo[i] = s.k_lo, q.k_len[i] = s.k_len, q.k_slot[i] = s.k_slot;
+            q.job0[i] = (int32_t)job0;
+            return i;
+        };
         for (size_t i = 0; i < n; ++i) {
             const Seq& s = seqs[first + i];
-            l.seqs.q_lo[i] = s.q_lo, l.seqs.q_len[i] = s.q_len, l.seqs.k_lo[i] = s.k_lo, l.seqs.k_len[i] = s.k_len, l.seqs.k_slot[i] = s.k_slot;
-            l.seqs.job0[i] = (int32_t)jobs;
-            jobs += jobs_of(s);
+            const int64_t tiles = tiles_of(s);
+            const int32_t runs = kmip::full_runs(streamed_of(s), p->split);
+            put(l.seqs, s, jobs);
+            if (runs > 1) {
+                l.part0[put(l.tiles, s, tile_jobs)] = (int32_t)jobs;
+                tile_jobs += tiles;
+                l.runs = std::max(l.runs, runs);
+            }
+            jobs += tiles * runs;
             if (p->jobs + jobs >= (int64_t(1) << 31) - 1) return record_error(KMIP_ERR_INVALID_ARG, "too many rows and key runs for one call");
         }
-        l.seqs.count = (int32_t)n;
         l.jobs = (int32_t)jobs;
+        l.tile_jobs = (int32_t)tile_jobs;
         l.first_job = (int32_t)p->jobs;
+        // two workgroups a CU are resident at once (see full_tile)
+        l.fold = causal && jobs <= 512;
         p->jobs += jobs;
-        p->launches.push_back(l);
     }
     return KMIP_OK;
 }
 
-// The forward's jobs.
-kmip_status_t plan_fwd(const Sequences& sq, int32_t H, int32_t Hk, FullPlan* p) {
+constexpr int64_t kSlots = 512;   // workgroups resident at once, two on each of 256 CUs
+
+int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
+
+// How `seqs` become tiles of kept rows, kept_of(s) of them for each key head, that
+// stream streamed_of(s) rows each.
+//   128 rows: waves share the streamed tiles, a quarter of the traffic; for
+//     tiles that are at least half full and fill the chip, by themselves or in runs
+//     of at least 512 streamed rows.
+//   32 rows otherwise, in runs of at least 512 where that makes more jobs.
+// Runs cost the sums' way through memory, so that there are as few as fill the chip.
+template <typename Kept, typename Streamed>
+kmip_status_t plan(std::vector<Seq>& seqs, int32_t Hk, bool causal, const Kept& kept_of, const Streamed& streamed_of, FullPlan* p) {
+    auto tiles = [&](const Seq& s, int64_t rows) { return (kept_of(s) + rows - 1) / rows * Hk; };
+    int64_t kept = 0, jobs = 0, work = 0, work32 = 0, longest = 0;
+    for (const Seq& s : seqs) {
+        kept += kept_of(s) * Hk;
+        jobs += tiles(s, 128);
+        work += tiles(s, 128) * streamed_of(s);
+        work32 += tiles(s, 32) * streamed_of(s);
+        longest = std::max<int64_t>(longest, streamed_of(s));
+    }
+    const bool full = 2 * kept >= 128 * jobs;
+    p->rows = full && (jobs >= kSlots || work >= kSlots * 512) ? 128 : 32;
+    int64_t run = 0;
+    if (p->rows == 32)
+        run = std::max<int64_t>(round_up(work32 / (2 * kSlots), 128), 512);
+    else if (jobs < kSlots)
+        run = std::max<int64_t>(round_up(work / kSlots, 128), 512);
+    p->split = run > 0 && longest >= 2 * run ? (int32_t)std::min<int64_t>(run, INT32_MAX) : 0;
+    return cut(seqs, causal, [&](const Seq& s) { return tiles(s, p->rows); }, streamed_of, p);
+}
+
+kmip_status_t plan_rows(const Sequences& sq, int32_t H, int32_t Hk, bool causal, FullPlan* p) {
     const int64_t rep = H / Hk;
     std::vector<Seq> seqs;
-    int64_t rows = 0, keys = 0; // keys: over all row tiles of 32
-    for (int32_t g = 0; g < sq.count; ++g) {
-        const Seq s = sq.at(g);
-        if (s.q_len == 0) continue;
-        seqs.push_back(s);
-        const int64_t t = (s.q_len * rep + 31) / 32 * Hk;
-        rows += s.q_len * rep * Hk;
-        keys += t * s.k_len;
-    }
-    // Tiles of 128 rows once they fill the chip's 256 CUs
-    p->rows = rows >= 256 * 128 ? 128 : 32;
-    p->split = 0;
-    if (p->rows == 32) {
-        // runs of keys such that there are about 1024 jobs of like length
-        const int64_t run = std::max<int64_t>((keys / 1024 + 127) / 128 * 128, 256);
-        for (const Seq& s : seqs)
-            if (s.k_len > run) p->split = (int32_t)run;
-    }
-    const int32_t R = p->rows, split = p->split;
-    auto runs = [=](const Seq& s) { return split > 0 && s.k_len > split ? (s.k_len + (int64_t)split - 1) / split : 1; };
-    kmip_status_t e = cut(seqs, [&](const Seq& s) { return (s.q_len * rep + R - 1) / R * Hk * runs(s); }, p);
-    if (e != KMIP_OK) return e;
-    if (split > 0)
-        for (FullLaunch& l : p->launches)
-            for (int32_t i = 0; i < l.seqs.count; ++i)
-                if (l.seqs.k_len[i] > split)
-                    l.split_rows = std::max<int32_t>(l.split_rows, (int32_t)std::min<int64_t>(32, l.seqs.q_len[i] * rep));
-    return KMIP_OK;
+    for (int32_t g = 0; g < sq.count; ++g)
+        if (sq.at(g).q_len > 0) seqs.push_back(sq.at(g));
+    return plan(seqs, Hk, causal, [=](const Seq& s) { return s.q_len * rep; }, [](const Seq& s) { return (int64_t)s.k_len; }, p);
 }
 
-// The backward's jobs: row tiles for dQ, key tiles for dK and dV (of every slot,
-// since rows without a gradient are written too).
-kmip_status_t plan_bwd(const Sequences& sq, int32_t H, int32_t Hk, FullPlan* dq, FullPlan* dkv) {
+// Key tiles cover every slot, since rows without a gradient are written too.
+kmip_status_t plan_keys(const Sequences& sq, int32_t H, int32_t Hk, bool causal, FullPlan* p) {
     const int64_t rep = H / Hk;
-    std::vector<Seq> rows, keys;
-    int64_t nrows = 0, nkeys = 0;
-    for (int32_t g = 0; g < sq.count; ++g) {
-        const Seq s = sq.at(g);
-        if (s.q_len > 0) rows.push_back(s);
-        if (s.k_slot > 0) keys.push_back(s);
-        nrows += s.q_len * rep * Hk;
-        nkeys += (int64_t)s.k_slot * Hk;
-    }
-    dq->rows = nrows >= 256 * 128 ? 128 : 32;
-    dkv->rows = nkeys >= 256 * 128 ? 128 : 32;
-    const int32_t R = dq->rows, S = dkv->rows;
-    kmip_status_t e = cut(rows, [=](const Seq& s) { return (s.q_len * rep + R - 1) / R * Hk; }, dq);
-    if (e != KMIP_OK) return e;
-    return cut(keys, [=](const Seq& s) { return ((int64_t)s.k_slot + S - 1) / S * Hk; }, dkv);
+    std::vector<Seq> seqs;
+    for (int32_t g = 0; g < sq.count; ++g)
+        if (sq.at(g).k_slot > 0) seqs.push_back(sq.at(g));
+    return plan(seqs, Hk, causal, [](const Seq& s) { return (int64_t)s.k_slot; }, [=](const Seq& s) { return s.q_len * rep; }, p);
 }
 
 // Workspace of the forward: the runs' sums, then their maxima and sums of weights.
@@ -176,6 +186,23 @@ FwdLayout fwd_layout(const FullPlan& p, int32_t dv) {
     const size_t rows = (size_t)p.jobs * p.rows;
     const size_t ml = align_up(rows * dv * sizeof(float));
     return FwdLayout{ml, ml + align_up(rows * 2 * sizeof(float))};
+}
+
+// Workspace of the backward: lse2 and D, then the runs' sums of dQ, dK and dV.
+struct BwdLayout {
+    size_t D, dq, dk, dv, total;
+};
+BwdLayout bwd_layout(const FullPlan& dq, const FullPlan& dkv, int64_t Nq, int32_t H, int32_t d, int32_t dv) {
+    BwdLayout L;
+    auto sums = [](const FullPlan& p, int32_t width) {
+        return p.split == 0 ? (size_t)0 : align_up((size_t)p.jobs * p.rows * width * sizeof(float));
+    };
+    L.D = align_up((size_t)Nq * H * sizeof(float));
+    L.dq = 2 * L.D;
+    L.dk = L.dq + sums(dq, d);
+    L.dv = L.dk + sums(dkv, d);
+    L.total = L.dv + sums(dkv, dv);
+    return L;
 }
 
 // A stride in values between rows of a 16-bit tensor that the kernels read 16
@@ -236,7 +263,7 @@ size_t kmip_full_fwd_workspace_size(const int32_t* q_offsets, const int32_t* k_o
         Sequences sq;
         FullPlan p;
         kmip_status_t e = check_call(q_offsets, k_offsets, k_lengths, num_seqs, Nq, Nk, H, Hk, d, dv, &sq);
-        if (e == KMIP_OK) e = plan_fwd(sq, H, Hk, &p);
+        if (e == KMIP_OK) e = plan_rows(sq, H, Hk, false, &p);
         if (e == KMIP_OK) bytes = fwd_layout(p, dv).total;
         return e;
     });
@@ -258,7 +285,7 @@ kmip_status_t kmip_full_fwd(const void* Q, const void* K, const void* V, int32_t
         if (e == KMIP_OK) e = fill_call(Q, K, V, dtype, strides, Nq, Nk, H, Hk, d, dv, scale, causal, &f);
         if (e == KMIP_OK && Nq > 0 && (reinterpret_cast<uintptr_t>(out) & 15u) != 0)
             e = record_error(KMIP_ERR_INVALID_ARG, "out must be 16-byte aligned");
-        if (e == KMIP_OK) e = plan_fwd(sq, H, Hk, &p);
+        if (e == KMIP_OK) e = plan_rows(sq, H, Hk, causal != 0, &p);
         if (e != KMIP_OK) return e;
         const FwdLayout L = fwd_layout(p, dv);
         if ((e = check_workspace(workspace, workspace_bytes, L.total)) != KMIP_OK) return e;
@@ -274,9 +301,17 @@ kmip_status_t kmip_full_fwd(const void* Q, const void* K, const void* V, int32_t
 
 size_t kmip_full_bwd_workspace_size(const int32_t* q_offsets, const int32_t* k_offsets, const int32_t* k_lengths,
                                     int32_t num_seqs, int64_t Nq, int64_t Nk, int32_t H, int32_t Hk, int32_t d, int32_t dv) {
-    Sequences sq;
-    if (check_call(q_offsets, k_offsets, k_lengths, num_seqs, Nq, Nk, H, Hk, d, dv, &sq) != KMIP_OK) return 0;
-    return align_up((size_t)Nq * H * sizeof(float));
+    size_t bytes = 0;
+    guarded([&]() {
+        Sequences sq;
+        FullPlan dq, dkv;
+        kmip_status_t e = check_call(q_offsets, k_offsets, k_lengths, num_seqs, Nq, Nk, H, Hk, d, dv, &sq);
+        if (e == KMIP_OK) e = plan_rows(sq, H, Hk, false, &dq);
+        if (e == KMIP_OK) e = plan_keys(sq, H, Hk, false, &dkv);
+        if (e == KMIP_OK) bytes = bwd_layout(dq, dkv, Nq, H, d, dv).total;
+        return e;
+    });
+    return bytes;
 }
 
 kmip_status_t kmip_full_bwd(const void* Q, const void* K, const void* V, const void* dOut, const void* out,
@@ -298,12 +333,16 @@ kmip_status_t kmip_full_bwd(const void* Q, const void* K, const void* V, const v
         for (const void* p : {out, static_cast<const void*>(dQ), static_cast<const void*>(dK), static_cast<const void*>(dV)})
             if (e == KMIP_OK && (reinterpret_cast<uintptr_t>(p) & 15u) != 0)
                 e = record_error(KMIP_ERR_INVALID_ARG, "out, dQ, dK and dV must be 16-byte aligned");
-        if (e == KMIP_OK) e = check_workspace(workspace, workspace_bytes, align_up((size_t)Nq * H * sizeof(float)));
-        if (e == KMIP_OK) e = plan_bwd(sq, H, Hk, &dq, &dkv);
+        if (e == KMIP_OK) e = plan_rows(sq, H, Hk, causal != 0, &dq);
+        if (e == KMIP_OK) e = plan_keys(sq, H, Hk, causal != 0, &dkv);
         if (e != KMIP_OK) return e;
+        const BwdLayout L = bwd_layout(dq, dkv, Nq, H, d, dv);
+        if ((e = check_workspace(workspace, workspace_bytes, L.total)) != KMIP_OK) return e;
         f.dout = dOut, f.out_in = out, f.lse_in = lse;
         f.dq = dQ, f.dk = dK, f.dv_out = dV;
-        hipError_t h = kmip::launch_full_bwd(f, dq, dkv, reinterpret_cast<float*>(workspace), reinterpret_cast<hipStream_t>(stream));
+        auto at = [&](size_t off) { return reinterpret_cast<float*>(reinterpret_cast<char*>(workspace) + off); };
+        const kmip::FullBwdSpace ws{at(0), at(L.D), at(L.dq), at(L.dk), at(L.dv)};
+        hipError_t h = kmip::launch_full_bwd(f, dq, dkv, ws, reinterpret_cast<hipStream_t>(stream));
         return h == hipSuccess ? ok() : hip_fail(h, "full attention backward launch");
     });
 }

@@ -21,11 +21,14 @@ struct BwdArgs {
     const char *q, *k, *v, *dout;
     const uint16_t* out;
     const float* lse;
-    float* D;
+    float *lse2, *D;                          // [Nq, H]: lse log2 e (+inf for a row that sees no key), D
     uint16_t *dq, *dk, *dv_out;
+    float *part_dq, *part_dk, *part_dv;       // runs: [job][rows][width] sums
     int64_t q_row, q_head, k_row, k_head, v_row, v_head, do_row, do_head;   // bytes between tokens, heads
-    int32_t H, Hk, rep, d, dv, causal;
+    int32_t H, Hk, rep, d, dv, split;
+    bool causal, fold;
     float scale;
+    int32_t first_job;
     FullSeqs s;
 };
 
@@ -34,11 +37,12 @@ __global__ __launch_bounds__(256, ROWS == 128 ? 2 : 1) void full_dq_kernel(const
     constexpr int kTile = ROWS == 128 ? (D == 16 ? 128 : 64) : 32;
     constexpr int kBytes = kTile * 2 * D;
     constexpr int kWaves = 4, kOwn = ROWS == 128 ? 1 : kWaves;
+    constexpr int kBufs = ROWS == 128 ? 2 : kStages<D>;
     constexpr int kT = D < 32 ? 1 : D / 32;
-    __shared__ __attribute__((aligned(1024))) char sh[kOwn * 4 * kBytes];
+    __shared__ __attribute__((aligned(1024))) char sh[kOwn * kBufs * 2 * kBytes];
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const RowJob j = row_job<ROWS>(a.s, a.Hk, a.rep, a.causal, 0, blockIdx.x, lane);
+    const RowJob j = row_job<ROWS>(a.s, a.Hk, a.rep, a.causal, a.fold, a.split, blockIdx.x, lane);
     const int32_t nrows = j.q_len * a.rep;
     const int32_t row0 = j.tile * ROWS + (ROWS == 128 ? 32 * wave : 0);
     const int32_t off = j.k_len - j.q_len;
@@ -65,16 +69,22 @@ __global__ __launch_bounds__(256, ROWS == 128 ? 2 : 1) void full_dq_kernel(const
         const float2 ds = both_halves(di);
         di = ds.x + ds.y;
     }
-    if (live && lane < 32 && (ROWS == 128 || wave == 0)) a.D[at] = di;
     const float lse = a.lse[at];
     // a row that sees no key: every weight 0
     const float lse2 = lse == -INFINITY ? INFINITY : lse * kLog2e;
+    if (live && lane < 32 && (ROWS == 128 || wave == 0) && j.run == 0) {
+        a.lse2[at] = lse2;
+        a.D[at] = di;
+    }
     const float c = a.scale * kLog2e;
-    const int32_t lim = sees(row), lim_first = sees(row0), lim_last = sees(row0 + 31), hi = sees(j.tile * ROWS + ROWS - 1);
+    const int32_t lim = sees(row), lim_first = sees(row0), lim_last = sees(row0 + 31);
+    const int32_t lo = a.split > 0 ? j.run * a.split : 0;
+    int32_t hi = sees(j.tile * ROWS + ROWS - 1);
+    if (j.runs > 1) hi = min(hi, lo + a.split);
 
     const char* kp = a.k + (int64_t)j.k_lo * a.k_row + j.kv_head * a.k_head;
     const char* vp = a.v + (int64_t)j.k_lo * a.v_row + j.kv_head * a.v_head;
-    const uint32_t base = lds_addr(sh) + (ROWS == 128 ? 0 : wave * 4 * kBytes);
+    const uint32_t base = lds_addr(sh) + (ROWS == 128 ? 0 : wave * kBufs * 2 * kBytes);
     constexpr int kParts = ROWS == 128 ? kWaves : 1;
     const int part = ROWS == 128 ? wave : 0;
     TileLoad<D, kParts> kl, vl;
@@ -121,35 +131,33 @@ __global__ __launch_bounds__(256, ROWS == 128 ? 2 : 1) void full_dq_kernel(const
         }
     };
     if constexpr (ROWS == 128) {
-        if (hi > 0) fetch(0, 0);
+        if (lo < hi) fetch(lo, 0);
         int buf = 0;
-        for (int32_t key = 0; key < hi; key += kTile, buf ^= 1) {
+        for (int32_t key = lo; key < hi; key += kTile, buf ^= 1) {
             wait_and_sync();
             if (key + kTile < hi) fetch(key + kTile, buf ^ 1);
             if (key < lim_last) compute(key, buf);
         }
         if (!live) return;
+        const int64_t job = (int64_t)a.first_job + blockIdx.x;
 #pragma unroll
-        for (int t = 0; t < kT; ++t) store_piece<T>(a.dq + at * a.d, acc[t], t, a.scale, a.d, lane);
-    } else {
-        constexpr int kLoads = 2 * kTile / TileLoad<D, 1>::kPer;
-        int32_t key = 32 * wave;
-        if (key < hi) fetch(key, 0);
-        for (int buf = 0; key < hi; key += 32 * kWaves, buf ^= 1) {
-            if (key + 32 * kWaves < hi) {
-                wait_lds();   // the reads of that buffer
-                fetch(key + 32 * kWaves, buf ^ 1);
-                wait_loads<kLoads>();
-            } else {
-                wait_loads<0>();
-            }
-            compute(key, buf);
+        for (int t = 0; t < kT; ++t) {
+            if (j.runs > 1)
+                store_sums(a.part_dq + (job * ROWS + (row - j.tile * ROWS)) * a.d, acc[t], t, a.d, lane);
+            else
+                store_piece<T>(a.dq + at * a.d, acc[t], t, a.scale, a.d, lane);
         }
+    } else {
+        // blocks lo + 32 (wave + 4 i)
+        const int32_t mine = lo + 32 * wave, n = mine < hi ? (hi - mine + 32 * kWaves - 1) / (32 * kWaves) : 0;
+        stream_blocks<kBufs, 2 * kTile / TileLoad<D, 1>::kPer>(
+            n, [&](int32_t i, int stage) { fetch(mine + 32 * kWaves * i, stage); },
+            [&](int32_t i, int stage) { compute(mine + 32 * kWaves * i, stage); });
         // the four waves' sums, in their order
         wait_and_sync();
         float* const so = reinterpret_cast<float*>(sh);
 #pragma unroll
-        for (int t = 0; t < kT; ++t) put_piece<D>(so + wave * 32 * D, acc[t], t, a.scale, lane);
+        for (int t = 0; t < kT; ++t) put_piece<D>(so + wave * 32 * D, acc[t], t, 1.0f, lane);
         wait_and_sync();
         for (int i = threadIdx.x; i < 32 * (D / 4); i += 256) {
             const int rr = i / (D / 4), gg = i % (D / 4);
@@ -159,38 +167,47 @@ __global__ __launch_bounds__(256, ROWS == 128 ? 2 : 1) void full_dq_kernel(const
 #pragma unroll
             for (int u = 1; u < kWaves; ++u) x += get_piece<D>(so + u * 32 * D, rr, gg);
             const int64_t to = (j.q_lo + (int64_t)(rowi / a.rep)) * a.H + j.kv_head * a.rep + rowi % a.rep;
-            s16x4 y;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) y[e] = T::round(x[e]);
-            *reinterpret_cast<s16x4*>(a.dq + to * a.d + 4 * gg) = y;
+            if (j.runs > 1)
+                *reinterpret_cast<f32x4*>(a.part_dq + (((int64_t)a.first_job + blockIdx.x) * ROWS + rr) * a.d + 4 * gg) = x;
+            else
+                *reinterpret_cast<s16x4*>(a.dq + to * a.d + 4 * gg) = round4<T>(x, a.scale);
         }
     }
 }
 
 template <typename T, int D, int KEYS>
-__global__ __launch_bounds__(256, KEYS == 128 && D < 128 ? 2 : 1) void full_dkv_kernel(const BwdArgs a) {
-    constexpr int kTile = KEYS == 128 ? (D == 16 ? 128 : 64) : 32;   // tokens a buffer holds
+__global__ __launch_bounds__(256, KEYS == 128 ? 2 : 1) void full_dkv_kernel(const BwdArgs a) {
+    constexpr int kTile = KEYS == 128 ? (D == 16 ? 128 : D == 128 ? 32 : 64) : 32;   // tokens a buffer holds
+    constexpr bool kHeld = KEYS == 32 || D < 128;   // V in registers, else in LDS
     constexpr int kBytes = kTile * 2 * D;
     constexpr int kWaves = 4, kOwn = KEYS == 128 ? 1 : kWaves;
+    constexpr int kBufs = KEYS == 128 ? 2 : kStages<D>;
     constexpr int kT = D < 32 ? 1 : D / 32;
-    __shared__ __attribute__((aligned(1024))) char sh[kOwn * 4 * kBytes];       // [buffer][Q, dout]
-    __shared__ __attribute__((aligned(16))) float st[kOwn][2][2][kTile];       // [buffer][lse log2 e, D]
+    __shared__ __attribute__((aligned(1024))) char sh[kOwn * kBufs * 2 * kBytes];   // [buffer][Q, dout]
+    __shared__ __attribute__((aligned(1024))) char shv[kHeld ? 1024 : KEYS * 2 * D];   // V of the kept keys
+    __shared__ __attribute__((aligned(16))) float st[kOwn][kBufs][2][kTile];   // [buffer][lse log2 e, D]
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int sq = __builtin_amdgcn_readfirstlane(seq_of_job(a.s, blockIdx.x, lane));
     const int32_t q_lo = a.s.q_lo[sq], q_len = a.s.q_len[sq], k_lo = a.s.k_lo[sq], k_len = a.s.k_len[sq], slot = a.s.k_slot[sq];
-    const int32_t kv_head = (blockIdx.x - a.s.job0[sq]) % a.Hk, tile = (blockIdx.x - a.s.job0[sq]) / a.Hk;
+    const int32_t runs = full_runs((int64_t)q_len * a.rep, a.split), kv_head = (blockIdx.x - a.s.job0[sq]) % a.Hk;
+    const int32_t rest = (blockIdx.x - a.s.job0[sq]) / a.Hk, run = rest % runs;
+    const int32_t tile = full_tile(rest / runs, (slot - 1) / KEYS + 1, a.causal, true, a.fold);
     const int32_t off = k_len - q_len;
     const int32_t tile_lo = tile * KEYS;                       // keys from here on
     const int32_t key0 = tile_lo + (KEYS == 128 ? 32 * wave : 0), key = key0 + (lane & 31);
     const int64_t key_at = min(key, max(k_len, 1) - 1);
-    s16x8 k[D / 16], v[D / 16];
+    s16x8 k[D / 16], v[kHeld ? D / 16 : 1];
     if (k_len > 0) {
         load_columns<D>(k, a.k + (k_lo + key_at) * a.k_row + kv_head * a.k_head, a.d, lane);
-        load_columns<D>(v, a.v + (k_lo + key_at) * a.v_row + kv_head * a.v_head, a.dv, lane);
+        if constexpr (kHeld) load_columns<D>(v, a.v + (k_lo + key_at) * a.v_row + kv_head * a.v_head, a.dv, lane);
     } else {
 #pragma unroll
-        for (int t = 0; t < D / 16; ++t) k[t] = v[t] = s16x8{};
+        for (int t = 0; t < D / 16; ++t) k[t] = s16x8{};
+        if constexpr (kHeld) {
+#pragma unroll
+            for (int t = 0; t < D / 16; ++t) v[t] = s16x8{};
+        }
     }
     // the first token that sees the tile, and its first and last key of this wave
     const int32_t t_lo = tile_lo >= k_len ? q_len : a.causal ? max(0, tile_lo - off) : 0;
@@ -200,31 +217,28 @@ __global__ __launch_bounds__(256, KEYS == 128 && D < 128 ? 2 : 1) void full_dkv_
     f32x16 dk[kT], dv[kT];
 #pragma unroll
     for (int t = 0; t < kT; ++t) clear(dk[t]), clear(dv[t]);
-    const uint32_t base = lds_addr(sh) + (KEYS == 128 ? 0 : wave * 4 * kBytes);
+    const uint32_t base = lds_addr(sh) + (KEYS == 128 ? 0 : wave * kBufs * 2 * kBytes);
     float(*const stats)[2][kTile] = st[KEYS == 128 ? 0 : wave];
     constexpr int kParts = KEYS == 128 ? kWaves : 1;
     const int part = KEYS == 128 ? wave : 0;
     TileLoad<D, kParts> ql, gl;
     ql.init(lane, part, a.d, (uint32_t)a.q_row);
     gl.init(lane, part, a.dv, (uint32_t)a.do_row);
+    const uint32_t st_base = lds_addr(stats);
     auto fetch = [&](int32_t hr, int32_t tok, int buf) {
         const int32_t head = kv_head * a.rep + hr;
         ql.template issue<kTile>(base + buf * 2 * kBytes, a.q + (q_lo + (int64_t)tok) * a.q_row + head * a.q_head, part,
                                  q_len - tok);
         gl.template issue<kTile>(base + buf * 2 * kBytes + kBytes, a.dout + (q_lo + (int64_t)tok) * a.do_row + head * a.do_head,
                                  part, q_len - tok);
-    };
-    // one token's lse log2 e and D; a token behind the last, or one that sees no
-    // key, has weights 0 through an infinite lse
-    auto stat = [&](int32_t hr, int32_t tok, int i) {
-        float2 x = make_float2(INFINITY, 0.0f);
-        if (tok + i < q_len) {
-            const int64_t at = (q_lo + (int64_t)(tok + i)) * a.H + kv_head * a.rep + hr;
-            const float lse = a.lse[at], di = a.D[at];
-            if (lse != -INFINITY) x = make_float2(lse * kLog2e, di);
+        // the tokens' statistics, 64 values a wave
+        if (part < kTile / 32) {
+            const int i = 64 * part + lane;
+            const int64_t at = (q_lo + (int64_t)min(tok + i % kTile, q_len - 1)) * a.H + head;
+            load_word_to_lds(st_base + buf * kTile * 8 + 256 * part, (i < kTile ? a.lse2 : a.D) + at);
         }
-        return x;
     };
+    const uint32_t kept_v = kHeld ? 0 : row_operand<D>(lds_addr(shv) + wave * 64 * D, lane);
     auto compute = [&](int32_t tok, int buf) {
         const uint32_t qt = base + buf * 2 * kBytes;
         const uint32_t qa = row_operand<D>(qt, lane), ga = row_operand<D>(qt + kBytes, lane);
@@ -239,10 +253,14 @@ __global__ __launch_bounds__(256, KEYS == 128 && D < 128 ? 2 : 1) void full_dkv_
 #pragma unroll
             for (int t = 0; t < D / 16; ++t) s = T::mfma(lds_row16((qa ^ (32 * t)) + b * 64 * D), k[t], s);
 #pragma unroll
-            for (int t = 0; t < D / 16; ++t) dp = T::mfma(lds_row16((ga ^ (32 * t)) + b * 64 * D), v[t], dp);
+            for (int t = 0; t < D / 16; ++t) {
+                if (!kHeld && 16 * t >= a.dv) break;   // (neither side has zeros there)
+                dp = T::mfma(lds_row16((ga ^ (32 * t)) + b * 64 * D), kHeld ? v[kHeld ? t : 0] : lds_row16(kept_v ^ (32 * t)), dp);
+            }
             const float* sb = &stats[buf][0][32 * b + 4 * (lane >> 5)];
-            const bool edge = tok + 32 * b < t_all;
-            const int32_t from = a.causal ? key - off - tok - 32 * b - 4 * (lane >> 5) : 0;   // first row that sees the key
+            // rows of the block that see the key; those behind the last token do not
+            const bool edge = tok + 32 * b < t_all || tok + 32 * b + 32 > q_len;
+            const int32_t from = a.causal ? key - off - tok - 32 * b - 4 * (lane >> 5) : 0, upto = q_len - tok - 32 * b - 4 * (lane >> 5);
 #pragma unroll
             for (int r = 0; r < 16; r += 4) {
                 const f32x4 l = *reinterpret_cast<const f32x4*>(sb + 2 * r), di = *reinterpret_cast<const f32x4*>(sb + kTile + 2 * r);
@@ -250,7 +268,7 @@ __global__ __launch_bounds__(256, KEYS == 128 && D < 128 ? 2 : 1) void full_dkv_
                 for (int e = 0; e < 4; ++e) {
                     float p = __builtin_amdgcn_exp2f(fmaf(s[r + e], c, -l[e]));
                     float x = p * (dp[r + e] - di[e]);
-                    if (edge && e + 2 * r < from) p = 0.0f, x = 0.0f;
+                    if (edge && (e + 2 * r < from || e + 2 * r >= upto)) p = 0.0f, x = 0.0f;
                     s[r + e] = p;
                     dp[r + e] = x;
                 }
@@ -268,35 +286,35 @@ __global__ __launch_bounds__(256, KEYS == 128 && D < 128 ? 2 : 1) void full_dkv_
         }
     };
 
-    // tiles: rep heads of `per` tiles each
+    // streamed tiles: rep heads of `per` each; this run's part of them
     const int32_t per = (q_len - t_lo + kTile - 1) / kTile;
-    const int32_t n = t_lo < q_len ? per * a.rep : 0;
-    if constexpr (KEYS == 128) {
-        int32_t hr = 0, tok = t_lo;
+    const int64_t all = t_lo < q_len ? (int64_t)per * a.rep : 0;
+    const int32_t first = (int32_t)(all * run / runs), n = (int32_t)(all * (run + 1) / runs) - first;
+    const int64_t job = (int64_t)a.first_job + blockIdx.x;
+    if constexpr (!kHeld) {
         if (n > 0) {
-            fetch(0, tok, 0);
-            if (threadIdx.x < kTile) {
-                const float2 x = stat(0, tok, threadIdx.x);
-                stats[0][0][threadIdx.x] = x.x;
-                stats[0][1][threadIdx.x] = x.y;
-            }
+            TileLoad<D, kWaves> vl;
+            vl.init(lane, wave, a.dv, (uint32_t)a.v_row);
+            vl.template issue<KEYS>(lds_addr(shv), a.v + (k_lo + (int64_t)tile_lo) * a.v_row + kv_head * a.v_head, wave, k_len - tile_lo);
+        }
+    }
+    if constexpr (KEYS == 128) {
+        int32_t hr = 0, tok = 0;
+        if (n > 0) {
+            hr = first / per;
+            tok = t_lo + first % per * kTile;
+            fetch(hr, tok, 0);
         }
         for (int32_t i = 0; i < n; ++i) {
             const int buf = i & 1;
             const int32_t now = tok;
             wait_and_sync();
-            float2 x = make_float2(0.0f, 0.0f);
             if (i + 1 < n) {
                 tok += kTile;
                 if (tok >= q_len) tok = t_lo, ++hr;
-                if (threadIdx.x < kTile) x = stat(hr, tok, threadIdx.x);
                 fetch(hr, tok, buf ^ 1);
             }
             if (now + kTile > t_wave) compute(now, buf);
-            if (i + 1 < n && threadIdx.x < kTile) {
-                stats[buf ^ 1][0][threadIdx.x] = x.x;
-                stats[buf ^ 1][1][threadIdx.x] = x.y;
-            }
         }
         if (key >= slot) return;
         const int64_t at = (k_lo + (int64_t)key) * a.Hk + kv_head;
@@ -305,36 +323,21 @@ __global__ __launch_bounds__(256, KEYS == 128 && D < 128 ? 2 : 1) void full_dkv_
 #pragma unroll
         for (int t = 0; t < kT; ++t) {
             if (!used) clear(dk[t]), clear(dv[t]);
+            if (runs > 1) {
+                store_sums(a.part_dk + (job * KEYS + (key - tile_lo)) * a.d, dk[t], t, a.d, lane);
+                store_sums(a.part_dv + (job * KEYS + (key - tile_lo)) * a.dv, dv[t], t, a.dv, lane);
+                continue;
+            }
             store_piece<T>(a.dk + at * a.d, dk[t], t, a.scale, a.d, lane);
             store_piece<T>(a.dv_out + at * a.dv, dv[t], t, 1.0f, a.dv, lane);
         }
     } else {
-        constexpr int kLoads = 2 * kTile / TileLoad<D, 1>::kPer;
-        auto place = [&](int32_t i, int32_t* hr, int32_t* tok) {
-            *hr = i / per;
-            *tok = t_lo + (i % per) * kTile;
-        };
-        int32_t hr = 0, tok = 0;
-        float2 x = make_float2(0.0f, 0.0f);
-        if (wave < n) {
-            place(wave, &hr, &tok);
-            x = stat(hr, tok, lane & 31);
-            fetch(hr, tok, 0);
-        }
-        for (int32_t i = wave, buf = 0; i < n; i += kWaves, buf ^= 1) {
-            const int32_t now = tok;
-            if (lane < 32) stats[buf][0][lane] = x.x, stats[buf][1][lane] = x.y;
-            wait_lds();   // the reads of the other buffer, and this write
-            if (i + kWaves < n) {
-                place(i + kWaves, &hr, &tok);
-                x = stat(hr, tok, lane & 31);
-                fetch(hr, tok, buf ^ 1);
-                wait_loads<kLoads>();
-            } else {
-                wait_loads<0>();
-            }
-            compute(now, buf);
-        }
+        // tiles first + wave + 4 i
+        const int32_t mine = n > wave ? (n - wave + kWaves - 1) / kWaves : 0;
+        auto tok_of = [&](int32_t i) { return t_lo + (first + wave + kWaves * i) % per * kTile; };
+        stream_blocks<kBufs, 2 * kTile / TileLoad<D, 1>::kPer + 1>(
+            mine, [&](int32_t i, int stage) { fetch((first + wave + kWaves * i) / per, tok_of(i), stage); },
+            [&](int32_t i, int stage) { compute(tok_of(i), stage); });
         // the four waves' sums, in their order: dK, then dV
         float* const so = reinterpret_cast<float*>(sh);
 #pragma unroll
@@ -342,7 +345,7 @@ __global__ __launch_bounds__(256, KEYS == 128 && D < 128 ? 2 : 1) void full_dkv_
             const int32_t width = w == 0 ? a.d : a.dv;
             wait_and_sync();
 #pragma unroll
-            for (int t = 0; t < kT; ++t) put_piece<D>(so + wave * 32 * D, w == 0 ? dk[t] : dv[t], t, w == 0 ? a.scale : 1.0f, lane);
+            for (int t = 0; t < kT; ++t) put_piece<D>(so + wave * 32 * D, w == 0 ? dk[t] : dv[t], t, 1.0f, lane);
             wait_and_sync();
             for (int i = threadIdx.x; i < 32 * (D / 4); i += 256) {
                 const int rr = i / (D / 4), gg = i % (D / 4);
@@ -350,18 +353,65 @@ __global__ __launch_bounds__(256, KEYS == 128 && D < 128 ? 2 : 1) void full_dkv_
                 f32x4 y = get_piece<D>(so, rr, gg);
 #pragma unroll
                 for (int u = 1; u < kWaves; ++u) y += get_piece<D>(so + u * 32 * D, rr, gg);
-                s16x4 z;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) z[e] = T::round(tile_lo + rr < k_len ? y[e] : 0.0f);
+                if (tile_lo + rr >= k_len) y = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+                if (runs > 1) {
+                    *reinterpret_cast<f32x4*>((w == 0 ? a.part_dk : a.part_dv) + (job * KEYS + rr) * width + 4 * gg) = y;
+                    continue;
+                }
                 uint16_t* to = w == 0 ? a.dk : a.dv_out;
-                *reinterpret_cast<s16x4*>(to + ((k_lo + (int64_t)(tile_lo + rr)) * a.Hk + kv_head) * width + 4 * gg) = z;
+                *reinterpret_cast<s16x4*>(to + ((k_lo + (int64_t)(tile_lo + rr)) * a.Hk + kv_head) * width + 4 * gg) =
+                    round4<T>(y, w == 0 ? a.scale : 1.0f);
             }
         }
     }
 }
 
+struct SumArgs {
+    const float* part;          // [job][rows][width]
+    uint16_t* to;
+    FullSeqs s;                 // the sequences with several runs, a job for each tile and key head
+    int32_t part0[kFullSeqs];
+    int32_t first_job, rows, width, split, Hk, rep;
+    bool causal, fold, keys;    // keys: rows are keys of the slot, else (token, head) pairs
+    float scale;
+};
+
+// Adds the runs of a tile in their order.
+template <typename T>
+__global__ __launch_bounds__(256) void full_sum_kernel(const SumArgs a) {
+    const int s = __builtin_amdgcn_readfirstlane(seq_of_job(a.s, blockIdx.x, threadIdx.x & 63));
+    const int32_t nrows = a.keys ? a.s.k_slot[s] : a.s.q_len[s] * a.rep;
+    const int32_t runs = full_runs(a.keys ? (int64_t)a.s.q_len[s] * a.rep : a.s.k_len[s], a.split);
+    const int32_t kv_head = (blockIdx.x - a.s.job0[s]) % a.Hk, place = (blockIdx.x - a.s.job0[s]) / a.Hk;
+    const int32_t tile = full_tile(place, (nrows - 1) / a.rows + 1, a.causal, a.keys, a.fold);
+    const int groups = a.width / 4;
+    const int i = blockIdx.y * 256 + threadIdx.x, rr = i / groups, g = i % groups;
+    const int32_t row = tile * a.rows + rr;
+    if (rr >= a.rows || row >= nrows) return;
+    const float* p = a.part + (((int64_t)a.first_job + a.part0[s] + (int64_t)place * runs * a.Hk + kv_head) * a.rows + rr) * a.width + 4 * g;
+    const int64_t step = (int64_t)a.Hk * a.rows * a.width;
+    f32x4 x = *reinterpret_cast<const f32x4*>(p);
+#pragma unroll 4
+    for (int32_t r = 1; r < runs; ++r) x += *reinterpret_cast<const f32x4*>(p + r * step);
+    const int64_t at = a.keys ? (a.s.k_lo[s] + (int64_t)row) * a.Hk + kv_head
+                              : (a.s.q_lo[s] + (int64_t)(row / a.rep)) * (a.Hk * a.rep) + kv_head * a.rep + row % a.rep;
+    *reinterpret_cast<s16x4*>(a.to + at * a.width + 4 * g) = round4<T>(x, a.scale);
+}
+
+template <typename T>
+hipError_t launch_sum(const BwdArgs& a, const FullLaunch& l, const FullPlan& p, const float* part, uint16_t* to, int32_t width,
+                      bool keys, float scale, hipStream_t stream) {
+    SumArgs b{};
+    b.part = part, b.to = to, b.s = l.tiles;
+    for (int i = 0; i < kFullSeqs; ++i) b.part0[i] = l.part0[i];
+    b.first_job = l.first_job, b.rows = p.rows, b.width = width, b.split = p.split, b.Hk = a.Hk, b.rep = a.rep;
+    b.causal = a.causal, b.fold = l.fold, b.keys = keys, b.scale = scale;
+    hipLaunchKernelGGL((full_sum_kernel<T>), dim3(l.tile_jobs, (p.rows * (width / 4) + 255) / 256), dim3(256), 0, stream, b);
+    return hipGetLastError();
+}
+
 template <typename T, int D>
-hipError_t launch_bwd(const FullCall& f, const FullPlan& dq, const FullPlan& dkv, float* Dv, hipStream_t stream) {
+hipError_t launch_bwd(const FullCall& f, const FullPlan& dq, const FullPlan& dkv, const FullBwdSpace& ws, hipStream_t stream) {
     BwdArgs a{};
     a.q = reinterpret_cast<const char*>(f.q);
     a.k = reinterpret_cast<const char*>(f.k);
@@ -369,7 +419,8 @@ hipError_t launch_bwd(const FullCall& f, const FullPlan& dq, const FullPlan& dkv
     a.dout = reinterpret_cast<const char*>(f.dout);
     a.out = reinterpret_cast<const uint16_t*>(f.out_in);
     a.lse = f.lse_in;
-    a.D = Dv;
+    a.lse2 = ws.lse2, a.D = ws.D;
+    a.part_dq = ws.dq, a.part_dk = ws.dk, a.part_dv = ws.dv;
     a.dq = reinterpret_cast<uint16_t*>(f.dq);
     a.dk = reinterpret_cast<uint16_t*>(f.dk);
     a.dv_out = reinterpret_cast<uint16_t*>(f.dv_out);
@@ -377,24 +428,27 @@ hipError_t launch_bwd(const FullCall& f, const FullPlan& dq, const FullPlan& dkv
     a.k_row = 2 * f.k_row, a.k_head = 2 * f.k_head;
     a.v_row = 2 * f.v_row, a.v_head = 2 * f.v_head;
     a.do_row = 2 * f.do_row, a.do_head = 2 * f.do_head;
-    a.H = f.H, a.Hk = f.Hk, a.rep = f.H / f.Hk, a.d = f.d, a.dv = f.dv, a.causal = f.causal;
+    a.H = f.H, a.Hk = f.Hk, a.rep = f.H / f.Hk, a.d = f.d, a.dv = f.dv, a.causal = f.causal != 0;
     a.scale = f.scale;
     for (const FullLaunch& l : dq.launches) {
-        a.s = l.seqs;
+        a.s = l.seqs, a.first_job = l.first_job, a.fold = l.fold, a.split = dq.split;
         if (dq.rows == 128)
             hipLaunchKernelGGL((full_dq_kernel<T, D, 128>), dim3(l.jobs), dim3(256), 0, stream, a);
         else
             hipLaunchKernelGGL((full_dq_kernel<T, D, 32>), dim3(l.jobs), dim3(256), 0, stream, a);
-        const hipError_t e = hipGetLastError();
+        hipError_t e = hipGetLastError();
+        if (e == hipSuccess && l.tile_jobs > 0) e = launch_sum<T>(a, l, dq, ws.dq, a.dq, f.d, false, f.scale, stream);
         if (e != hipSuccess) return e;
     }
     for (const FullLaunch& l : dkv.launches) {
-        a.s = l.seqs;
+        a.s = l.seqs, a.first_job = l.first_job, a.fold = l.fold, a.split = dkv.split;
         if (dkv.rows == 128)
             hipLaunchKernelGGL((full_dkv_kernel<T, D, 128>), dim3(l.jobs), dim3(256), 0, stream, a);
         else
             hipLaunchKernelGGL((full_dkv_kernel<T, D, 32>), dim3(l.jobs), dim3(256), 0, stream, a);
-        const hipError_t e = hipGetLastError();
+        hipError_t e = hipGetLastError();
+        if (e == hipSuccess && l.tile_jobs > 0) e = launch_sum<T>(a, l, dkv, ws.dk, a.dk, f.d, true, f.scale, stream);
+        if (e == hipSuccess && l.tile_jobs > 0) e = launch_sum<T>(a, l, dkv, ws.dv, a.dv_out, f.dv, true, 1.0f, stream);
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
@@ -402,10 +456,10 @@ hipError_t launch_bwd(const FullCall& f, const FullPlan& dq, const FullPlan& dkv
 
 }  // namespace
 
-hipError_t launch_full_bwd(const FullCall& f, const FullPlan& dq, const FullPlan& dkv, float* D, hipStream_t stream) {
+hipError_t launch_full_bwd(const FullCall& f, const FullPlan& dq, const FullPlan& dkv, const FullBwdSpace& ws, hipStream_t stream) {
     const int32_t w = f.d > f.dv ? f.d : f.dv;
 #define KMIP_FULL_BWD(W) \
-    if (w == W) return f.fp16 ? launch_bwd<Fp16, W>(f, dq, dkv, D, stream) : launch_bwd<Bf16, W>(f, dq, dkv, D, stream);
+    if (w == W) return f.fp16 ? launch_bwd<Fp16, W>(f, dq, dkv, ws, stream) : launch_bwd<Bf16, W>(f, dq, dkv, ws, stream);
     KMIP_FULL_BWD(16)
     KMIP_FULL_BWD(32)
     KMIP_FULL_BWD(64)

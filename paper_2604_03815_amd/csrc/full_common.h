@@ -118,6 +118,11 @@ __device__ __forceinline__ void load_to_lds(uint32_t lds, const char* base, uint
     __builtin_amdgcn_global_load_lds((const KMIP_GLOBAL void*)(base + off), (KMIP_LDS void*)(uintptr_t)lds, 16, 0, 0);
 }
 
+// The same with 4 bytes a lane, each from an address of its own.
+__device__ __forceinline__ void load_word_to_lds(uint32_t lds, const float* p) {
+    __builtin_amdgcn_global_load_lds((const KMIP_GLOBAL void*)p, (KMIP_LDS void*)(uintptr_t)lds, 4, 0, 0);
+}
+
 // All but the last n loads of this wave have ended.
 template <int N>
 __device__ __forceinline__ void wait_loads() {
@@ -195,7 +200,7 @@ struct RowJob {
 };
 
 template <int ROWS>
-__device__ __forceinline__ RowJob row_job(const FullSeqs& seqs, int32_t Hk, int32_t rep, int32_t causal, int32_t split,
+__device__ __forceinline__ RowJob row_job(const FullSeqs& seqs, int32_t Hk, int32_t rep, bool causal, bool fold, int32_t split,
                                           int32_t job, int lane) {
     const int s = __builtin_amdgcn_readfirstlane(seq_of_job(seqs, job, lane));
     RowJob j;
@@ -203,7 +208,7 @@ __device__ __forceinline__ RowJob row_job(const FullSeqs& seqs, int32_t Hk, int3
     j.q_len = seqs.q_len[s];
     j.k_lo = seqs.k_lo[s];
     j.k_len = seqs.k_len[s];
-    j.runs = split > 0 && j.k_len > split ? (j.k_len - 1) / split + 1 : 1;
+    j.runs = full_runs(j.k_len, split);
     const int32_t tiles = (int32_t)(((int64_t)j.q_len * rep + ROWS - 1) / ROWS);
     // key heads first: with 8 of them (or a divisor) workgroups of one XCD,
     // which come round robin, share a head's keys in its L2
@@ -211,9 +216,7 @@ __device__ __forceinline__ RowJob row_job(const FullSeqs& seqs, int32_t Hk, int3
     j.kv_head = rest % Hk;
     rest /= Hk;
     j.run = rest % j.runs;
-    // causal: the tiles with the most keys first
-    j.tile = rest / j.runs;
-    if (causal) j.tile = tiles - 1 - j.tile;
+    j.tile = full_tile(rest / j.runs, tiles, causal, false, fold);
     return j;
 }
 
@@ -258,6 +261,49 @@ __device__ __forceinline__ void store_piece(uint16_t* row, const f32x16& x, int 
             for (int e = 0; e < 4; ++e) y[e] = T::round(x[r + e] * f);
             *reinterpret_cast<s16x4*>(row + col) = y;
         }
+    }
+}
+
+// The same in float32, unrounded (a run's sums).
+__device__ __forceinline__ void store_sums(float* row, const f32x16& x, int t, int32_t cols, int lane) {
+#pragma unroll
+    for (int r = 0; r < 16; r += 4) {
+        const int col = 32 * t + 2 * r + 4 * (lane >> 5);
+        if (col < cols) *reinterpret_cast<f32x4*>(row + col) = f32x4{x[r], x[r + 1], x[r + 2], x[r + 3]};
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ s16x4 round4(const f32x4& x, float f) {
+    s16x4 y;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = T::round(x[e] * f);
+    return y;
+}
+
+// Stages of LDS that a wave with buffers of its own keeps (two tensors of 32
+// rows each, 128 D bytes): deep enough for the loads' latency where a block
+// takes little time, few enough for several workgroups a CU.
+template <int D>
+constexpr int kStages = D == 16 ? 4 : D == 32 ? 3 : 2;
+
+// A wave's own stream: `fetch(i, stage)` issues block i's loads (LOADS
+// instructions), `use(i, stage)` computes on it, for i < n.
+template <int STAGES, int LOADS, typename Fetch, typename Use>
+__device__ __forceinline__ void stream_blocks(int32_t n, const Fetch& fetch, const Use& use) {
+    static_assert((STAGES - 1) * LOADS < 64, "counted by vmcnt");
+#pragma unroll
+    for (int i = 0; i < STAGES - 1; ++i)
+        if (i < n) fetch(i, i);
+    for (int32_t i = 0, stage = 0; i < n; ++i, stage = stage + 1 == STAGES ? 0 : stage + 1) {
+        if (i + STAGES - 1 < n) {
+            wait_lds();   // the reads of the stage that is filled again
+            fetch(i + STAGES - 1, stage == 0 ? STAGES - 1 : stage - 1);
+            wait_loads<(STAGES - 1) * LOADS>();
+        } else {
+            wait_loads<0>();
+        }
+        use(i, stage);
     }
 }
 

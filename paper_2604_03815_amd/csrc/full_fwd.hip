@@ -32,7 +32,8 @@ struct FwdArgs {
     float* lse;
     float *part_o, *part_ml;    // split: [job][ROWS][dv] sums, [job][ROWS][2] maximum (times c) and sum
     int64_t q_row, q_head, k_row, k_head, v_row, v_head;   // bytes between tokens, heads
-    int32_t H, Hk, rep, d, dv, causal, split;
+    int32_t H, Hk, rep, d, dv, split;
+    bool causal, fold;
     float scale;
     int32_t first_job;          // of the launch, among the call's
     FullSeqs s;
@@ -115,12 +116,13 @@ __global__ __launch_bounds__(256, ROWS == 128 ? 2 : 1) void full_fwd_kernel(cons
     constexpr int kTile = ROWS == 128 ? (D == 16 ? 128 : 64) : 32;   // keys a buffer holds
     constexpr int kBytes = kTile * 2 * D;                            // of one tensor's buffer
     constexpr int kWaves = 4, kOwn = ROWS == 128 ? 1 : kWaves;       // buffer sets
+    constexpr int kBufs = ROWS == 128 ? 2 : kStages<D>;
     constexpr int kT = FwdWave<T, D>::kT;
-    __shared__ __attribute__((aligned(1024))) char sh[kOwn * 4 * kBytes];
-    static_assert(ROWS == 128 || kOwn * 4 * kBytes >= 32 * D * 4 * kWaves, "room for the join");
+    __shared__ __attribute__((aligned(1024))) char sh[kOwn * kBufs * 2 * kBytes];
+    static_assert(ROWS == 128 || sizeof(sh) >= 32 * D * 4 * kWaves, "room for the join");
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const RowJob j = row_job<ROWS>(a.s, a.Hk, a.rep, a.causal, a.split, blockIdx.x, lane);
+    const RowJob j = row_job<ROWS>(a.s, a.Hk, a.rep, a.causal, a.fold, a.split, blockIdx.x, lane);
     const int32_t nrows = j.q_len * a.rep;
     const int32_t row0 = j.tile * ROWS + (ROWS == 128 ? 32 * wave : 0);
     const int32_t off = j.k_len - j.q_len;
@@ -147,7 +149,7 @@ __global__ __launch_bounds__(256, ROWS == 128 ? 2 : 1) void full_fwd_kernel(cons
     const float c = a.scale * kLog2e;
     const char* kp = a.k + (int64_t)j.k_lo * a.k_row + j.kv_head * a.k_head;
     const char* vp = a.v + (int64_t)j.k_lo * a.v_row + j.kv_head * a.v_head;
-    const uint32_t base = lds_addr(sh) + (ROWS == 128 ? 0 : wave * 4 * kBytes);   // [buffer][K, V]
+    const uint32_t base = lds_addr(sh) + (ROWS == 128 ? 0 : wave * kBufs * 2 * kBytes);   // [buffer][K, V]
     constexpr int kParts = ROWS == 128 ? kWaves : 1;
     const int part = ROWS == 128 ? wave : 0;
     TileLoad<D, kParts> kl, vl;
@@ -172,19 +174,11 @@ __global__ __launch_bounds__(256, ROWS == 128 ? 2 : 1) void full_fwd_kernel(cons
             if (key < lim_last) compute(key, buf);
         }
     } else {
-        constexpr int kLoads = 2 * kTile / TileLoad<D, 1>::kPer;
-        int32_t key = lo + 32 * wave;
-        if (key < hi) fetch(key, 0);
-        for (int buf = 0; key < hi; key += 32 * kWaves, buf ^= 1) {
-            if (key + 32 * kWaves < hi) {
-                wait_lds();   // the reads of that buffer
-                fetch(key + 32 * kWaves, buf ^ 1);
-                wait_loads<kLoads>();
-            } else {
-                wait_loads<0>();
-            }
-            compute(key, buf);
-        }
+        // blocks lo + 32 (wave + 4 i)
+        const int32_t mine = lo + 32 * wave, n = mine < hi ? (hi - mine + 32 * kWaves - 1) / (32 * kWaves) : 0;
+        stream_blocks<kBufs, 2 * kTile / TileLoad<D, 1>::kPer>(
+            n, [&](int32_t i, int stage) { fetch(mine + 32 * kWaves * i, stage); },
+            [&](int32_t i, int stage) { compute(mine + 32 * kWaves * i, stage); });
     }
 
     const float2 ls = both_halves(w.l);
@@ -197,12 +191,7 @@ __global__ __launch_bounds__(256, ROWS == 128 ? 2 : 1) void full_fwd_kernel(cons
         if (j.runs > 1) {
             float* po = a.part_o + (job * ROWS + (row - j.tile * ROWS)) * a.dv;
 #pragma unroll
-            for (int t = 0; t < kT; ++t)
-#pragma unroll
-                for (int r = 0; r < 16; r += 4) {
-                    const int col = 32 * t + 8 * (r >> 2) + 4 * h;
-                    if (col < a.dv) *reinterpret_cast<f32x4*>(po + col) = f32x4{w.o[t][r], w.o[t][r + 1], w.o[t][r + 2], w.o[t][r + 3]};
-                }
+            for (int t = 0; t < kT; ++t) store_sums(po, w.o[t], t, a.dv, lane);
             if (h == 0) {
                 float* ml = a.part_ml + (job * ROWS + (row - j.tile * ROWS)) * 2;
                 ml[0] = mc;
@@ -258,63 +247,66 @@ __global__ __launch_bounds__(256, ROWS == 128 ? 2 : 1) void full_fwd_kernel(cons
             }
             const int64_t at = (j.q_lo + (int64_t)(rowi / a.rep)) * a.H + j.kv_head * a.rep + rowi % a.rep;
             const float inv = ll > 0.0f ? 1.0f / ll : 0.0f;
-            s16x4 y;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) y[e] = T::round(x[e] * inv);
-            *reinterpret_cast<s16x4*>(a.out + at * a.dv + 4 * g) = y;
+            *reinterpret_cast<s16x4*>(a.out + at * a.dv + 4 * g) = round4<T>(x, inv);
             if (g == 0) a.lse[at] = ll > 0.0f ? (mm + __builtin_amdgcn_logf(ll)) * kLn2 : -INFINITY;
         }
     }
 }
 
-// Joins the runs of a row tile's keys: one workgroup a row.  Threads take
-// (run, four columns); the runs' sums are added in the order of the runs
-// within a thread, then over the threads of a column in a fixed order.
-template <typename T, int ROWS>
-__global__ __launch_bounds__(256) void full_join_kernel(const FwdArgs a) {
+struct JoinArgs {
+    FwdArgs f;                  // f.s: the sequences with several runs, a job for each tile and key head
+    int32_t part0[kFullSeqs];   // their first jobs' places among the sums
+    int32_t rows;               // of a tile
+    int32_t lanes;              // threads that share a row's four columns, a power of two
+};
+
+// Joins the runs of row tiles.  A thread takes four columns of a row
+// and every lanes-th run; its sum, then the threads' in order.
+template <typename T>
+__global__ __launch_bounds__(256) void full_join_kernel(const JoinArgs b) {
+    const int32_t ROWS = b.rows;
+    const FwdArgs& a = b.f;
     __shared__ f32x4 part[256];
-    __shared__ float wm[4], wl[4];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const RowJob j = row_job<ROWS>(a.s, a.Hk, a.rep, a.causal, a.split, blockIdx.x, lane);
-    if (j.runs == 1 || j.run != 0) return;
-    const int32_t row = j.tile * ROWS + blockIdx.y;
-    if (row >= j.q_len * a.rep) return;
-    const int64_t job = (int64_t)a.first_job + blockIdx.x;   // run 0; run r is r * Hk jobs on
-    const float* ml = a.part_ml + (job * ROWS + blockIdx.y) * 2;
+    __shared__ float sm[256], sl[256];
+    const int s = __builtin_amdgcn_readfirstlane(seq_of_job(a.s, blockIdx.x, threadIdx.x & 63));
+    const int32_t q_lo = a.s.q_lo[s], nrows = a.s.q_len[s] * a.rep, runs = full_runs(a.s.k_len[s], a.split);
+    const int32_t tiles = (nrows + ROWS - 1) / ROWS, kv_head = (blockIdx.x - a.s.job0[s]) % a.Hk, place = (blockIdx.x - a.s.job0[s]) / a.Hk;
+    const int32_t tile = full_tile(place, tiles, a.causal, false, a.fold);
+    const int groups = a.dv / 4;
+    const int g = threadIdx.x % groups, t = threadIdx.x / groups % b.lanes, rr = threadIdx.x / groups / b.lanes + blockIdx.y * (256 / groups / b.lanes);
+    const int32_t row = tile * ROWS + rr;
+    const bool live = rr < ROWS && row < nrows;
+    // run 0; run r is r * Hk jobs on
+    const int64_t job = (int64_t)a.first_job + b.part0[s] + (int64_t)place * runs * a.Hk + kv_head;
+    const float2* ml = reinterpret_cast<const float2*>(a.part_ml) + job * ROWS + rr;
+    const float* po = a.part_o + (job * ROWS + rr) * a.dv + 4 * g;
     const int64_t step = (int64_t)a.Hk * ROWS;
-    float top = -INFINITY, sum = 0.0f;
-    for (int32_t r = threadIdx.x; r < j.runs; r += 256) top = fmaxf(top, ml[r * step * 2]);
-#pragma unroll
-    for (int s = 1; s < 64; s <<= 1) top = fmaxf(top, __shfl_xor(top, s));
-    if (lane == 0) wm[wave] = top;
+    float top = -INFINITY;
+    if (live)
+        for (int32_t r = t; r < runs; r += b.lanes) top = fmaxf(top, ml[r * step].x);
+    sm[threadIdx.x] = top;
     __syncthreads();
-    top = fmaxf(fmaxf(wm[0], wm[1]), fmaxf(wm[2], wm[3]));
-    for (int32_t r = threadIdx.x; r < j.runs; r += 256) {
-        const float l = ml[r * step * 2 + 1];
-        if (l > 0.0f) sum += l * __builtin_amdgcn_exp2f(ml[r * step * 2] - top);
-    }
-#pragma unroll
-    for (int s = 1; s < 64; s <<= 1) sum += __shfl_xor(sum, s);
-    if (lane == 0) wl[wave] = sum;
-    const int groups = a.dv / 4, lanes = 256 / groups;   // 4 .. 32 column groups, 64 .. 8 threads each
-    const int g = threadIdx.x % groups, t = threadIdx.x / groups;
-    const float* po = a.part_o + (job * ROWS + blockIdx.y) * a.dv + 4 * g;
+    const int first = threadIdx.x - t * groups;
+    for (int u = 0; u < b.lanes; ++u) top = fmaxf(top, sm[first + u * groups]);
     f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int32_t r = t; r < j.runs; r += lanes) {
-        if (ml[r * step * 2 + 1] > 0.0f)
-            x += __builtin_amdgcn_exp2f(ml[r * step * 2] - top) * *reinterpret_cast<const f32x4*>(po + r * step * a.dv);
-    }
+    float sum = 0.0f;
+    if (live && top != -INFINITY)
+        for (int32_t r = t; r < runs; r += b.lanes) {
+            const float2 m = ml[r * step];
+            const float f = __builtin_amdgcn_exp2f(m.x - top);
+            sum = fmaf(m.y, f, sum);
+            x += f * *reinterpret_cast<const f32x4*>(po + r * step * a.dv);
+        }
     part[threadIdx.x] = x;
+    sl[threadIdx.x] = sum;
     __syncthreads();
-    if (t != 0) return;
-    for (int u = 1; u < lanes; ++u) x += part[u * groups + g];
-    sum = (wl[0] + wl[1]) + (wl[2] + wl[3]);
-    const int64_t at = (j.q_lo + (int64_t)(row / a.rep)) * a.H + j.kv_head * a.rep + row % a.rep;
-    const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
-    s16x4 y;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) y[e] = T::round(x[e] * inv);
-    *reinterpret_cast<s16x4*>(a.out + at * a.dv + 4 * g) = y;
+    if (!live || t != 0) return;
+    for (int u = 1; u < b.lanes; ++u) {
+        x += part[threadIdx.x + u * groups];
+        sum += sl[threadIdx.x + u * groups];
+    }
+    const int64_t at = (q_lo + (int64_t)(row / a.rep)) * a.H + kv_head * a.rep + row % a.rep;
+    *reinterpret_cast<s16x4*>(a.out + at * a.dv + 4 * g) = round4<T>(x, sum > 0.0f ? 1.0f / sum : 0.0f);
     if (g == 0) a.lse[at] = sum > 0.0f ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
 }
 
@@ -331,20 +323,30 @@ hipError_t launch_fwd(const FullCall& f, const FullPlan& p, float* part_o, float
     a.q_row = 2 * f.q_row, a.q_head = 2 * f.q_head;
     a.k_row = 2 * f.k_row, a.k_head = 2 * f.k_head;
     a.v_row = 2 * f.v_row, a.v_head = 2 * f.v_head;
-    a.H = f.H, a.Hk = f.Hk, a.rep = f.H / f.Hk, a.d = f.d, a.dv = f.dv, a.causal = f.causal;
+    a.H = f.H, a.Hk = f.Hk, a.rep = f.H / f.Hk, a.d = f.d, a.dv = f.dv, a.causal = f.causal != 0;
     a.split = p.split;
     a.scale = f.scale;
     for (const FullLaunch& l : p.launches) {
         a.s = l.seqs;
         a.first_job = l.first_job;
+        a.fold = l.fold;
         if (p.rows == 128)
             hipLaunchKernelGGL((full_fwd_kernel<T, D, 128>), dim3(l.jobs), dim3(256), 0, stream, a);
         else
             hipLaunchKernelGGL((full_fwd_kernel<T, D, 32>), dim3(l.jobs), dim3(256), 0, stream, a);
         hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
-        if (l.split_rows > 0) {
-            hipLaunchKernelGGL((full_join_kernel<T, 32>), dim3(l.jobs, l.split_rows), dim3(256), 0, stream, a);
+        if (l.tile_jobs > 0) {
+            JoinArgs b{};
+            b.f = a;
+            b.f.s = l.tiles;
+            for (int i = 0; i < kFullSeqs; ++i) b.part0[i] = l.part0[i];
+            const int groups = f.dv / 4;
+            b.rows = p.rows;
+            b.lanes = 1;
+            while (2 * b.lanes <= l.runs && 2 * b.lanes * groups <= 256) b.lanes *= 2;
+            const int at_once = 256 / groups / b.lanes;   // rows a workgroup takes
+            hipLaunchKernelGGL((full_join_kernel<T>), dim3(l.tile_jobs, (p.rows + at_once - 1) / at_once), dim3(256), 0, stream, b);
             if ((e = hipGetLastError()) != hipSuccess) return e;
         }
     }

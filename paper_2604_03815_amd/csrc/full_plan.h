@@ -21,6 +21,21 @@ struct FullSeqs {
     int32_t count;
 };
 
+// Runs that the streamed rows of a tile are cut into.
+__host__ __device__ inline int32_t full_runs(int64_t streamed, int32_t split) {
+    return split > 0 && streamed > split ? (int32_t)((streamed - 1) / split + 1) : 1;
+}
+
+// Tile of place i of n.  Causal tiles differ in work; `falling`: tile 0 has the
+// most.  Most first while workgroups queue for the CUs.  Where all of them are
+// resident at once, the second half in the opposite order (fold), so that the
+// second workgroup of a CU is the shorter the longer its first one is.
+__host__ __device__ inline int32_t full_tile(int32_t i, int32_t n, bool causal, bool falling, bool fold) {
+    if (!causal) return i;
+    if (fold && i >= n / 2) i = n - 1 - (i - n / 2);
+    return falling ? i : n - 1 - i;
+}
+
 struct FullCall {
     const void *q, *k, *v, *dout, *out_in;
     void* out;
@@ -37,19 +52,28 @@ struct FullCall {
 struct FullLaunch {
     FullSeqs seqs;
     int32_t jobs, first_job;
-    int32_t split_rows;     // rows of the largest row tile whose keys are split, 0 if none is
+    bool fold;              // tiles in the order of full_tile()'s fold
+    // the launch that joins runs: the sequences that have several, with a job for
+    // each tile and key head; most runs among them
+    FullSeqs tiles;
+    int32_t part0[kFullSeqs];   // their first jobs in the launch above
+    int32_t tile_jobs, runs;
 };
 
 struct FullPlan {
-    int32_t rows = 0;    // rows of a row tile, 128 or 32
-    int32_t split = 0;   // keys of a run, 0: not split
+    int32_t rows = 0;    // rows (or keys) of a tile, 128 or 32
+    int32_t split = 0;   // streamed rows of a run, 0: not split
     int64_t jobs = 0;
     std::vector<FullLaunch> launches;
 };
 
-// dQ first (plan dq; it also writes D [Nq, H]), then dK and dV (plan dkv, rows: keys
-// of a job).
-hipError_t launch_full_bwd(const FullCall& f, const FullPlan& dq, const FullPlan& dkv, float* D, hipStream_t stream);
+// Workspace of the backward.
+struct FullBwdSpace {
+    float *lse2, *D;               // [Nq, H] each
+    float *dq, *dk, *dv;           // [job][rows][width] sums of runs
+};
+// dQ first (plan dq; it also writes lse2 and D), then dK and dV (plan dkv).
+hipError_t launch_full_bwd(const FullCall& f, const FullPlan& dq, const FullPlan& dkv, const FullBwdSpace& ws, hipStream_t stream);
 hipError_t launch_full_fwd(const FullCall& f, const FullPlan& p, float* part_o, float* part_ml, hipStream_t stream);
 
 }  // namespace kmip

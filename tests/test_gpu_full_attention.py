@@ -45,7 +45,11 @@ CASES = [
     # enough rows for tiles of 128
     (BF, 8, 8, 64, 64, [(4097, 4097)], True), (HF, 16, 4, 128, 128, [(700, 1300), (1500, 1500), (1, 9)], True),
     (BF, 16, 16, 32, 32, [(2100, 2100), (33, 129)], False), (BF, 33, 11, 16, 16, [(1000, 1000), (1, 64), (129, 1)], True),
-    (HF, 12, 4, 64, 128, [(3000, 2900)], True), (BF, 3, 3, 32, 32, [(n, n) for n in range(100, 451, 3)] , False),
+    (HF, 12, 4, 64, 128, [(3000, 2900)], True),
+    # tiles of 128 rows or keys whose streams are cut into runs
+    (BF, 8, 2, 128, 128, [(2048, 4096), (7, 100)], True), (BF, 4, 4, 128, 32, [(3001, 2999)], True),
+    (HF, 2, 1, 16, 128, [(5000, 6001)], False), (BF, 6, 2, 32, 32, [(900, 7000), (1, 5), (700, 1100)], True),
+    (BF, 1, 1, 16, 16, [(9001, 9001)], False), (HF, 8, 1, 64, 64, [(1500, 1500), (0, 300), (40, 0)], True), (BF, 3, 3, 32, 32, [(n, n) for n in range(100, 451, 3)] , False),
 ]
 
 
