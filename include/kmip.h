@@ -336,11 +336,13 @@ kmip_status_t kmip_fwd_noalloc(const void* Q, const void* K, const void* V, int6
  *  - NaN and Inf in the inputs give undefined (but memory-safe) results in the
  *    rows of their own sequence.
  *  - Nq * H and Nk below 2^31 - 4096; products of sizes and strides may pass 32 bits.
- *  - workspace: kmip_full_fwd_workspace_size() bytes (often 0: then NULL is
- *    taken), 256-byte aligned; the size depends on the offsets and lengths.
+ *  - workspace: kmip_full_fwd_workspace_size() bytes, 256-byte aligned; the size
+ *    depends on the offsets and lengths.  0 (then NULL is taken) where no sequence
+ *    has KMIP_FULL_LONG keys, and often else.
  *  - Results do not depend on the other sequences' values and are the same from
  *    call to call (no atomics).
  */
+#define KMIP_FULL_LONG 1024
 typedef enum { KMIP_BF16 = 0, KMIP_FP16 = 1, KMIP_FP32 = 2 } kmip_dtype_t;
 
 size_t kmip_full_fwd_workspace_size(const int32_t* q_offsets, const int32_t* k_offsets, const int32_t* k_lengths,

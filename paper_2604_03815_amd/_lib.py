@@ -31,6 +31,9 @@ EXPORTS = (
     "kmip_full_bwd_workspace_size", "kmip_full_bwd", "kmip_rotary", "kmip_status_string", "kmip_last_error",
 )
 
+# keys of a sequence below which kmip_full_fwd takes no workspace
+FULL_LONG = 1024
+
 # kmip_dtype_t
 BF16, FP16, FP32 = 0, 1, 2
 

@@ -156,6 +156,7 @@ kmip_status_t plan(std::vector<Seq>& seqs, int32_t Hk, bool causal, const Kept& 
         run = std::max<int64_t>(round_up(work32 / (2 * kSlots), 128), 512);
     else if (jobs < kSlots)
         run = std::max<int64_t>(round_up(work / kSlots, 128), 512);
+    static_assert(2 * 512 >= KMIP_FULL_LONG, "streams below are not cut");
     p->split = run > 0 && longest >= 2 * run ? (int32_t)std::min<int64_t>(run, INT32_MAX) : 0;
     return cut(seqs, causal, [&](const Seq& s) { return tiles(s, p->rows); }, streamed_of, p);
 }

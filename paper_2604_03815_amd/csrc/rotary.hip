@@ -6,7 +6,7 @@
 //
 // Angles: the frequency in turns a position is held as a 64-bit fraction, so
 // position * frequency modulo one turn is one wrapping integer product, exact
-// but for the fraction's own rounding (position * 2^-65 turns): far positions
+// but for the fraction's own rounding (position * 2^-63 turns): far positions
 // lose nothing.  Its top two bits (rounded) pick the quadrant; the rest, at most
 // pi/4, goes through the Taylor sums of sine and cosine (to x^9 and x^10:
 // remainders below 2e-9).  All in float32; the row's values are rounded once.
@@ -204,10 +204,10 @@ extern "C" kmip_status_t kmip_rotary(const void* X, void* Y, int32_t H, const vo
         uint64_t fb;
         std::memcpy(&fb, &freqs[i], sizeof(fb));
         if (((fb >> 52) & 0x7FF) == 0x7FF) return record_error(KMIP_ERR_INVALID_ARG, "freqs[%d] is not finite", i);
-        // the fraction of a turn (round to nearest; one whole turn wraps to 0)
-        const long double turns = (long double)freqs[i] / 6.283185307179586476925286766559005768L;
-        const long double part = turns - floorl(turns);
-        a.turns[i] = part >= 1.0L - 0x1p-65L ? 0 : (uint64_t)(part * 0x1p64L + 0.5L);
+        // the fraction of a turn, to 2^-63 (signed, so that it wraps)
+        const long double turns = (long double)freqs[i] * 0.15915494309189533576888376337251436L;
+        const long double part = turns < 0x1p62L && turns > -0x1p62L ? turns - (long double)(int64_t)turns : turns - floorl(turns);
+        a.turns[i] = (uint64_t)(int64_t)(part * 0x1p63L) << 1;
     }
     if (N == 0) return ok();
     if (!X || !Y || (H2 > 0 && (!X2 || !Y2))) return record_error(KMIP_ERR_INVALID_ARG, "null buffer passed to kmip_rotary");

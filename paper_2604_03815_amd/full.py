@@ -17,6 +17,7 @@ The offsets and lengths are read when the call is made: a captured call keeps th
 """
 from __future__ import annotations
 
+import array
 import ctypes
 import functools
 from typing import Optional, Sequence
@@ -24,31 +25,44 @@ from typing import Optional, Sequence
 import numpy as np
 import torch
 
-from ._lib import BF16, FP16, FP32, check, load
+from ._lib import BF16, FP16, FP32, FULL_LONG, check, load
 
 _DTYPES = {torch.bfloat16: BF16, torch.float16: FP16, torch.float32: FP32}
+_HALF = {torch.bfloat16: BF16, torch.float16: FP16}
 
 
-def _ptr(t):
-    return ctypes.c_void_p(0 if t is None else t.data_ptr())
-
-
-def _check_view(t, name, dtype, shape):
-    """A tensor of this type and shape whose last dimension is contiguous; returns its two other strides in values."""
+def _check_tensor(t, name, dtype, shape):
+    """A tensor of this type and shape whose last dimension is contiguous."""
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch tensor")
     if t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
-    if t.numel() and t.shape[-1] > 1 and t.stride(-1) != 1:
+    if not t.is_contiguous() and t.shape[-1] > 1 and t.stride(-1) != 1 and t.numel():
         raise ValueError(f"{name}: the last dimension must be contiguous")
-    return t.stride(0), t.stride(1)
+
+
+def _check_output(t, name, dtype, shape):
+    if t is not None:
+        _check_tensor(t, name, dtype, shape)
+        if not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous")
+
+
+def _strides(*tensors):
+    """Host int64 pairs of strides, or None where all are contiguous."""
+    if all(t.is_contiguous() for t in tensors):
+        return None
+    s = [x for t in tensors for x in t.stride()[:2]]
+    return (ctypes.c_int64 * len(s))(*s)
 
 
 def _check_devices(*named):
     dev = named[0][0].device
     for t, name in named:
+        if t is None:
+            continue
         if not t.is_cuda:
             raise TypeError(f"{name} must be a CUDA (HIP) tensor")
         if t.device != dev:
@@ -56,69 +70,66 @@ def _check_devices(*named):
     return dev
 
 
-class _on_device:
-    """The device of the tensors as the current one while a call launches, and its current stream."""
-
-    def __init__(self, device):
-        self.guard = torch.cuda.device(device) if torch.cuda.current_device() != device.index else None
-
-    def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
-        return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
-
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+def _launch(device, call, *args):
+    """call(*args, stream) with the tensors' device current, on its current stream."""
+    i = device.index
+    if torch._C._cuda_getDevice() == i:
+        check(call(*args, torch._C._cuda_getCurrentRawStream(i)))
+    else:
+        with torch.cuda.device(device):
+            check(call(*args, torch._C._cuda_getCurrentRawStream(i)))
 
 
-def _int32(values, name, n=None):
-    a = np.asarray(values)
-    if a.ndim != 1 or a.dtype.kind not in "iu" or (n is not None and len(a) != n) or (n is None and len(a) < 2):
-        raise ValueError(f"{name} must be a 1-D integer sequence of {n if n is not None else 'at least two'} entries")
-    if a.size and (a.min() < 0 or a.max() >= 1 << 31):
-        raise ValueError(f"{name} must lie in [0, 2^31)")
-    return np.ascontiguousarray(a, dtype=np.int32)
+class _Ints:
+    """A host int32 array of a 1-D integer sequence, and its address."""
+
+    __slots__ = ("keep", "ptr", "count", "most")
+
+    def __init__(self, values, name, n=None):
+        try:
+            if isinstance(values, (list, tuple)):
+                a = array.array("i", values)
+                self.ptr, self.count = a.buffer_info()
+            else:
+                a = np.asarray(values)
+                if a.ndim != 1 or a.dtype.kind not in "iu":
+                    raise TypeError
+                if a.size and (int(a.min()) < -(1 << 31) or int(a.max()) >= 1 << 31):
+                    raise OverflowError
+                a = np.ascontiguousarray(a, dtype=np.int32)
+                self.ptr, self.count = a.ctypes.data, len(a)
+        except (TypeError, OverflowError):
+            raise ValueError(f"{name} must be a 1-D sequence of 32-bit integers") from None
+        if self.count < 2 if n is None else self.count != n:
+            raise ValueError(f"{name} must have {'at least two' if n is None else n} entries, got {self.count}")
+        self.keep = a
 
 
 def _sequences(graph_offsets, key_offsets, key_lengths):
-    """Host arrays and their pointers, and the number of sequences."""
-    qo = None if graph_offsets is None else _int32(graph_offsets, "graph_offsets")
-    G = 1 if qo is None else len(qo) - 1
-    ko = None if key_offsets is None else _int32(key_offsets, "key_offsets", G + 1)
-    if qo is None and ko is not None:
+    """Host arrays (to be kept alive over the call), their addresses, the number of sequences."""
+    qo = None if graph_offsets is None else _Ints(graph_offsets, "graph_offsets")
+    G = 1 if qo is None else qo.count - 1
+    if qo is None and key_offsets is not None:
         raise ValueError("key_offsets needs graph_offsets")
-    kl = None if key_lengths is None else _int32(key_lengths, "key_lengths", G)
-    arrays = (qo, ko, kl)
-    return arrays, [ctypes.c_void_p(0 if a is None else a.ctypes.data) for a in arrays], G
+    ko = None if key_offsets is None else _Ints(key_offsets, "key_offsets", G + 1)
+    kl = None if key_lengths is None else _Ints(key_lengths, "key_lengths", G)
+    return (qo, ko, kl), tuple(None if a is None else a.ptr for a in (qo, ko, kl)), G
 
 
-def _sizes(q, k_, v):
+def _inputs(q, k_, v):
+    """Checks Q, K and V; returns (Nq, Nk, H, Hk, d, dv) and the dtype's code."""
     for t, name in ((q, "Q"), (k_, "K"), (v, "V")):
         if not isinstance(t, torch.Tensor) or t.dim() != 3:
             raise ValueError(f"{name} must be a tensor [N, heads, width]")
-    return q.shape[0], k_.shape[0], q.shape[1], k_.shape[1], q.shape[2], v.shape[2]
-
-
-def _inputs(q, k_, v, *more):
-    """Checks Q, K, V (and more (tensor, name, shape) of their type); returns sizes, strides (host int64) and dtype code."""
-    Nq, Nk, H, Hk, d, dv = _sizes(q, k_, v)
-    if q.dtype not in (torch.bfloat16, torch.float16):
+    code = _HALF.get(q.dtype)
+    if code is None:
         raise TypeError(f"Q must be torch.bfloat16 or torch.float16, got {q.dtype}")
-    strides = []
-    for t, name, shape in ((q, "Q", (Nq, H, d)), (k_, "K", (Nk, Hk, d)), (v, "V", (Nk, Hk, dv)), *more):
-        strides.extend(_check_view(t, name, q.dtype, shape))
-    return (Nq, Nk, H, Hk, d, dv), (ctypes.c_int64 * len(strides))(*strides), _DTYPES[q.dtype]
-
-
-def _output(t, name, dtype, shape, device):
-    """t (checked) or a new tensor."""
-    if t is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    _check_view(t, name, dtype, shape)
-    if not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
-    return t
+    Nq, H, d = q.shape
+    Nk, Hk, dv = v.shape
+    _check_tensor(q, "Q", q.dtype, (Nq, H, d))
+    _check_tensor(k_, "K", q.dtype, (Nk, Hk, d))
+    _check_tensor(v, "V", q.dtype, (Nk, Hk, dv))
+    return (Nq, Nk, H, Hk, d, dv), code
 
 
 def _scratch(workspace, nbytes, device):
@@ -132,6 +143,10 @@ def _scratch(workspace, nbytes, device):
     return buf
 
 
+def _address(t):
+    return None if t is None else t.data_ptr()
+
+
 def full_fwd_workspace_size(Nq: int, Nk: int, H: int, Hk: int, d: int, dv: int, graph_offsets=None, key_offsets=None,
                             key_lengths=None) -> int:
     keep, ptrs, G = _sequences(graph_offsets, key_offsets, key_lengths)
@@ -141,22 +156,22 @@ def full_fwd_workspace_size(Nq: int, Nk: int, H: int, Hk: int, d: int, dv: int, 
 def full_fwd(q, k_, v, scale: float, graph_offsets: Optional[Sequence[int]] = None, key_offsets=None, key_lengths=None,
              causal: bool = False, out=None, lse=None, workspace=None):
     """Full softmax attention: returns (out, lse)."""
-    (Nq, Nk, H, Hk, d, dv), strides, code = _inputs(q, k_, v)
-    given = [(t, n) for t, n in ((out, "out"), (lse, "lse")) if t is not None]
-    if out is not None:
-        _output(out, "out", q.dtype, (Nq, H, dv), None)
-    if lse is not None:
-        _output(lse, "lse", torch.float32, (Nq, H), None)
+    sizes, code = _inputs(q, k_, v)
+    Nq, Nk, H, Hk, d, dv = sizes
+    _check_output(out, "out", q.dtype, (Nq, H, dv))
+    _check_output(lse, "lse", torch.float32, (Nq, H))
     keep, ptrs, G = _sequences(graph_offsets, key_offsets, key_lengths)
-    dev = _check_devices((q, "Q"), (k_, "K"), (v, "V"), *given)
-    out = _output(out, "out", q.dtype, (Nq, H, dv), dev)
-    lse = _output(lse, "lse", torch.float32, (Nq, H), dev)
+    dev = _check_devices((q, "Q"), (k_, "K"), (v, "V"), (out, "out"), (lse, "lse"))
     lib = load()
-    buf = _scratch(workspace, lib.kmip_full_fwd_workspace_size(*ptrs, G, Nq, Nk, H, Hk, d, dv), dev)
-    with _on_device(dev) as stream:
-        check(lib.kmip_full_fwd(_ptr(q), _ptr(k_), _ptr(v), code, strides, *ptrs, G, Nq, Nk, H, Hk, d, dv, float(scale),
-                                int(bool(causal)), _ptr(out), _ptr(lse), _ptr(buf), 0 if buf is None else buf.numel(),
-                                stream))
+    buf = None
+    if Nk >= FULL_LONG:
+        buf = _scratch(workspace, lib.kmip_full_fwd_workspace_size(*ptrs, G, *sizes), dev)
+    if out is None:
+        out = torch.empty((Nq, H, dv), dtype=q.dtype, device=dev)
+    if lse is None:
+        lse = torch.empty((Nq, H), dtype=torch.float32, device=dev)
+    _launch(dev, lib.kmip_full_fwd, q.data_ptr(), k_.data_ptr(), v.data_ptr(), code, _strides(q, k_, v), *ptrs, G, *sizes, scale,
+            1 if causal else 0, out.data_ptr(), lse.data_ptr(), _address(buf), 0 if buf is None else buf.numel())
     return out, lse
 
 
@@ -169,21 +184,29 @@ def full_bwd_workspace_size(Nq: int, Nk: int, H: int, Hk: int, d: int, dv: int, 
 def full_bwd(q, k_, v, dout, out, lse, scale: float, graph_offsets: Optional[Sequence[int]] = None, key_offsets=None,
              key_lengths=None, causal: bool = False, dq=None, dk=None, dv=None, workspace=None):
     """Gradients of full softmax attention: returns (dQ, dK, dV) of the inputs' type."""
-    Nq, Nk, H, Hk, d, wv = _sizes(q, k_, v)
-    sizes, strides, code = _inputs(q, k_, v, (dout, "dOut", (Nq, H, wv)))
-    _output(out, "out", q.dtype, (Nq, H, wv), None)
-    _output(lse, "lse", torch.float32, (Nq, H), None)
-    shapes = ((dq, "dQ", (Nq, H, d)), (dk, "dK", (Nk, Hk, d)), (dv, "dV", (Nk, Hk, wv)))
-    given = [(t, n) for t, n, shape in shapes if t is not None and _output(t, n, q.dtype, shape, None) is not None]
+    sizes, code = _inputs(q, k_, v)
+    Nq, Nk, H, Hk, d, wv = sizes
+    _check_tensor(dout, "dOut", q.dtype, (Nq, H, wv))
+    for t, name, dtype, shape in ((out, "out", q.dtype, (Nq, H, wv)), (lse, "lse", torch.float32, (Nq, H))):
+        _check_tensor(t, name, dtype, shape)
+        _check_output(t, name, dtype, shape)
+    _check_output(dq, "dQ", q.dtype, (Nq, H, d))
+    _check_output(dk, "dK", q.dtype, (Nk, Hk, d))
+    _check_output(dv, "dV", q.dtype, (Nk, Hk, wv))
     keep, ptrs, G = _sequences(graph_offsets, key_offsets, key_lengths)
-    dev = _check_devices((q, "Q"), (k_, "K"), (v, "V"), (dout, "dOut"), (out, "out"), (lse, "lse"), *given)
-    dq, dk, dv = (_output(t, n, q.dtype, shape, dev) for t, n, shape in shapes)
+    dev = _check_devices((q, "Q"), (k_, "K"), (v, "V"), (dout, "dOut"), (out, "out"), (lse, "lse"), (dq, "dQ"), (dk, "dK"),
+                         (dv, "dV"))
     lib = load()
     buf = _scratch(workspace, lib.kmip_full_bwd_workspace_size(*ptrs, G, *sizes), dev)
-    with _on_device(dev) as stream:
-        check(lib.kmip_full_bwd(_ptr(q), _ptr(k_), _ptr(v), _ptr(dout), _ptr(out), _ptr(lse), code, strides, *ptrs, G,
-                                *sizes, float(scale), int(bool(causal)), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(buf),
-                                0 if buf is None else buf.numel(), stream))
+    if dq is None:
+        dq = torch.empty((Nq, H, d), dtype=q.dtype, device=dev)
+    if dk is None:
+        dk = torch.empty((Nk, Hk, d), dtype=q.dtype, device=dev)
+    if dv is None:
+        dv = torch.empty((Nk, Hk, wv), dtype=q.dtype, device=dev)
+    _launch(dev, lib.kmip_full_bwd, q.data_ptr(), k_.data_ptr(), v.data_ptr(), dout.data_ptr(), out.data_ptr(), lse.data_ptr(),
+            code, _strides(q, k_, v, dout), *ptrs, G, *sizes, scale, 1 if causal else 0, dq.data_ptr(), dk.data_ptr(),
+            dv.data_ptr(), _address(buf), 0 if buf is None else buf.numel())
     return dq, dk, dv
 
 

@@ -15,8 +15,8 @@ from typing import Optional
 import numpy as np
 import torch
 
-from ._lib import check, load
-from .full import _DTYPES, _check_devices, _check_view, _on_device, _ptr
+from ._lib import load
+from .full import _DTYPES, _address, _check_devices, _check_tensor, _launch as _launch_on
 
 
 def rotary_frequencies(rot: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0,
@@ -89,39 +89,44 @@ def _launch(q, k_, positions, freqs, interleaved, magnitude, inverse, dtype, q_o
     if k_ is not None:
         _rows(k_, "k")
         H2 = k_.shape[1]
+        _check_tensor(k_, "k", q.dtype, (N, H2, d))
     elif k_out is not None:
         raise ValueError("k_out without k")
+    _check_tensor(q, "q", q.dtype, (N, H, d))
     to = q.dtype if dtype is None else dtype
     if to not in _DTYPES:
         raise TypeError(f"dtype must be bfloat16, float16 or float32, got {to}")
-    strides, named = [], [(q, "q")]
-    for t, o, name, heads in ((q, q_out, "q", H), (k_, k_out, "k", H2)):
-        if t is None:
-            strides += [0] * 4
-            continue
-        strides += _check_view(t, name, q.dtype, (N, heads, d))
-        if o is None:
-            strides += [heads * d, d]
-        else:
-            s = _check_view(o, name + "_out", to, (N, heads, d))
-            if min(s[0] if N > 1 else d, s[1] if heads > 1 else d) < d:
-                raise ValueError(f"{name}_out overlaps itself")
-            strides += s
-            named.append((o, name + "_out"))
-        named.append((t, name))
+    _check_out(q_out, "q_out", to, (N, H, d))
+    _check_out(k_out, "k_out", to, (N, H2, d))
     if positions is not None:
         _check_positions(positions, N)
-        named.append((positions, "positions"))
-    dev = _check_devices(*named)
-    q_out = torch.empty((N, H, d), dtype=to, device=dev) if q_out is None else q_out
+    dev = _check_devices((q, "q"), (k_, "k"), (q_out, "q_out"), (k_out, "k_out"), (positions, "positions"))
+    if q_out is None:
+        q_out = torch.empty((N, H, d), dtype=to, device=dev)
     if k_ is not None and k_out is None:
         k_out = torch.empty((N, H2, d), dtype=to, device=dev)
-    host = (ctypes.c_int64 * 8)(*strides)
-    with _on_device(dev) as stream:
-        check(load().kmip_rotary(_ptr(q), _ptr(q_out), H, _ptr(k_), _ptr(k_out), H2, _DTYPES[q.dtype], _DTYPES[to], host,
-                                 _ptr(positions), ctypes.c_void_p(f.ctypes.data), N, d, 2 * len(f), int(bool(interleaved)),
-                                 float(magnitude), int(bool(inverse)), stream))
+    tensors = (q, q_out) if k_ is None else (q, q_out, k_, k_out)
+    strides = None
+    if not all(t.is_contiguous() for t in tensors):
+        s = [x for t in tensors for x in t.stride()[:2]]
+        strides = (ctypes.c_int64 * 8)(*s)
+    _launch_on(dev, load().kmip_rotary, q.data_ptr(), q_out.data_ptr(), H, _address(k_), _address(k_out), H2, _DTYPES[q.dtype],
+               _DTYPES[to], strides, _address(positions), f.ctypes.data, N, d, 2 * len(f), 1 if interleaved else 0, magnitude,
+               1 if inverse else 0)
     return q_out if k_ is None else (q_out, k_out)
+
+
+def _check_out(t, name, dtype, shape):
+    if t is None:
+        return
+    _check_tensor(t, name, dtype, shape)
+    N, heads, d = shape
+    if t.numel() and not t.is_contiguous():
+        rows, cols = (t.stride(0), N), (t.stride(1), heads)
+        # one of the two dimensions within the other's steps, rows of d values within the smaller's
+        inner, outer = sorted(x for x in (rows, cols) if x[1] > 1) if N > 1 and heads > 1 else ((d, 1), max(rows, cols, key=lambda x: x[1]))
+        if inner[0] < d or (outer[1] > 1 and outer[0] < (inner[1] - 1) * inner[0] + d):
+            raise ValueError(f"{name} overlaps itself")
 
 
 def _check_positions(positions, N):
