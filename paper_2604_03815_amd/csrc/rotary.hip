@@ -38,6 +38,7 @@ struct RotaryArgs {
     int32_t units, rot_units;         // threads a token and head group, those with pairs
     int32_t heads, first_heads, group;
     int32_t rot;
+    bool pass_by;
     float cos_scale, sin_scale;
     uint64_t turns[kMostPairs];
 };
@@ -58,24 +59,23 @@ struct Single {
     static __device__ __forceinline__ float round(float x) { return x; }
 };
 
-// P values of type T at p, aligned to their size or 16 bytes.
+// P values of type T, aligned to their size (at most 16 bytes).
 template <typename T, int P>
-struct alignas(sizeof(typename T::word) * P < 16 ? sizeof(typename T::word) * P : 16) Pack {
+struct alignas(sizeof(typename T::word) * P) Pack {
     typename T::word v[P];
 };
 
+// pass_by: past the caches, for results that do not fit them.
 template <typename T, int P>
-__device__ __forceinline__ void load(float (&x)[P], const char* p) {
-    const Pack<T, P> w = *reinterpret_cast<const Pack<T, P>*>(p);
-#pragma unroll
-    for (int e = 0; e < P; ++e) x[e] = T::widen(w.v[e]);
-}
-
-template <typename T, int P>
-__device__ __forceinline__ void store(char* p, const float (&x)[P]) {
-    Pack<T, P> w;
-#pragma unroll
-    for (int e = 0; e < P; ++e) w.v[e] = T::round(x[e]);
+__device__ __forceinline__ void put(char* p, const Pack<T, P>& w, bool pass_by) {
+    constexpr int kWords = sizeof(w) / 4;
+    if constexpr (kWords > 0) {
+        typedef uint32_t words __attribute__((ext_vector_type(kWords > 0 ? kWords : 1)));
+        if (pass_by) {
+            __builtin_nontemporal_store(__builtin_bit_cast(words, w), reinterpret_cast<words*>(p));
+            return;
+        }
+    }
     *reinterpret_cast<Pack<T, P>*>(p) = w;
 }
 
@@ -91,6 +91,31 @@ __device__ __forceinline__ void sin_cos(uint32_t phase, float* s, float* c) {
     *c = ((quarter + 1) & 2) ? -w : w;
 }
 
+// (u, v) of a thread turned: INTER with P > 1: P / 2 pairs in each, else pairs (u[e], v[e]).
+template <int P, bool INTER>
+__device__ __forceinline__ void turn(float (&u)[P], float (&v)[P], const float (&c)[P], const float (&s)[P]) {
+    auto pair = [](float& a, float& b, float cs, float sn) {
+        const float f = a * cs - b * sn;
+        b = b * cs + a * sn;
+        a = f;
+    };
+#pragma unroll
+    for (int e = 0; e < P; ++e) {
+        if constexpr (INTER && P > 1) {
+            if (e < P / 2)
+                pair(u[2 * e], u[2 * e + 1], c[e], s[e]);
+            else
+                pair(v[2 * e - P], v[2 * e - P + 1], c[e], s[e]);
+        } else {
+            pair(u[e], v[e], c[e], s[e]);
+        }
+    }
+}
+
+// Rows of a thread whose loads go out before the first store (which may write
+// the same memory, so that the compiler cannot move a load across it).
+constexpr int kRows = 4;
+
 template <typename TI, typename TO, int P, bool INTER>
 __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs a) {
     constexpr int kIn = sizeof(typename TI::word), kOut = sizeof(typename TO::word);
@@ -99,59 +124,55 @@ __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs a) {
     const uint32_t token = id / (uint32_t)a.units;
     const int unit = (int)(id - token * (uint32_t)a.units);
     const bool turned = unit < a.rot_units;
-    // first and second run of P values in the row
-    int one = 2 * P * unit, two = one + P;
+    // A thread's two runs of P values lie half of the turned (or of the passed
+    // on) dimensions apart: neighbouring threads touch neighbouring runs.
+    int one, two;
+    if (turned) {
+        one = P * unit, two = one + a.rot / 2;
+        if (INTER && P == 1) one = 2 * unit, two = one + 1;
+    } else {
+        one = a.rot + P * (unit - a.rot_units), two = one + P * (a.units - a.rot_units);
+    }
     float c[P], s[P];
     if (turned) {
-        if (!INTER) one = P * unit, two = one + a.rot / 2;
         const uint64_t pos = (uint64_t)(int64_t)(a.positions != nullptr ? a.positions[token] : (int32_t)token);
 #pragma unroll
         for (int e = 0; e < P; ++e) {
-            sin_cos((uint32_t)((pos * a.turns[P * unit + e]) >> 32), &s[e], &c[e]);
+            int i = P * unit + e;
+            if (INTER && P > 1) i = e < P / 2 ? one / 2 + e : two / 2 + e - P / 2;
+            sin_cos((uint32_t)((pos * a.turns[i]) >> 32), &s[e], &c[e]);
             c[e] *= a.cos_scale;
             s[e] *= a.sin_scale;
         }
-    } else {
-#pragma unroll
-        for (int e = 0; e < P; ++e) c[e] = 1.0f, s[e] = 0.0f;
     }
     const int h0 = blockIdx.y * a.group, h1 = min(h0 + a.group, a.heads);
-#pragma unroll 4
-    for (int h = h0; h < h1; ++h) {
-        const bool second = h >= a.first_heads;
-        const Side& t = a.s[second];
-        const int hh = second ? h - a.first_heads : h;
-        const char* x = t.x + (int64_t)token * t.x_row + hh * t.x_head;
-        char* y = t.y + (int64_t)token * t.y_row + hh * t.y_head;
-        float u[P], v[P], p[P], q[P];
-        load<TI, P>(u, x + one * kIn);
-        load<TI, P>(v, x + two * kIn);
-        if (!turned) {
-            store<TO, P>(y + one * kOut, u);
-            store<TO, P>(y + two * kOut, v);
-            continue;
+    for (int h = h0; h < h1; h += kRows) {
+        Pack<TI, P> x[kRows][2];
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+            if (h + r >= h1) break;
+            const bool second = h + r >= a.first_heads;
+            const Side& t = a.s[second];
+            const char* p = t.x + (int64_t)token * t.x_row + (second ? h + r - a.first_heads : h + r) * t.x_head;
+            x[r][0] = *reinterpret_cast<const Pack<TI, P>*>(p + one * kIn);
+            x[r][1] = *reinterpret_cast<const Pack<TI, P>*>(p + two * kIn);
         }
-        if constexpr (INTER) {   // u, v: 2 P neighbours
-            float w[2 * P];
 #pragma unroll
-            for (int e = 0; e < P; ++e) w[e] = u[e], w[P + e] = v[e];
+        for (int r = 0; r < kRows; ++r) {
+            if (h + r >= h1) break;
+            const bool second = h + r >= a.first_heads;
+            const Side& t = a.s[second];
+            char* y = t.y + (int64_t)token * t.y_row + (second ? h + r - a.first_heads : h + r) * t.y_head;
+            float u[P], v[P];
 #pragma unroll
-            for (int e = 0; e < P; ++e) {
-                const float f = w[2 * e] * c[e] - w[2 * e + 1] * s[e], g = w[2 * e + 1] * c[e] + w[2 * e] * s[e];
-                w[2 * e] = f;
-                w[2 * e + 1] = g;
-            }
+            for (int e = 0; e < P; ++e) u[e] = TI::widen(x[r][0].v[e]), v[e] = TI::widen(x[r][1].v[e]);
+            if (turned) turn<P, INTER>(u, v, c, s);
+            Pack<TO, P> w[2];
 #pragma unroll
-            for (int e = 0; e < P; ++e) p[e] = w[e], q[e] = w[P + e];
-        } else {
-#pragma unroll
-            for (int e = 0; e < P; ++e) {
-                p[e] = u[e] * c[e] - v[e] * s[e];
-                q[e] = v[e] * c[e] + u[e] * s[e];
-            }
+            for (int e = 0; e < P; ++e) w[0].v[e] = TO::round(u[e]), w[1].v[e] = TO::round(v[e]);
+            put(y + one * kOut, w[0], a.pass_by);
+            put(y + two * kOut, w[1], a.pass_by);
         }
-        store<TO, P>(y + one * kOut, p);
-        store<TO, P>(y + two * kOut, q);
     }
 }
 
@@ -168,7 +189,7 @@ void launch_types(const RotaryArgs& a, int pairs, bool inter, dim3 grid, hipStre
         else                                                                                                 \
             hipLaunchKernelGGL((rotary_kernel<TI, TO, P, false>), grid, dim3(256), 0, stream, a);            \
     }
-    KMIP_ROTARY(8)
+    if constexpr (sizeof(typename TI::word) == 2 && sizeof(typename TO::word) == 2) { KMIP_ROTARY(8) }
     KMIP_ROTARY(4)
     KMIP_ROTARY(1)
 #undef KMIP_ROTARY
@@ -214,20 +235,18 @@ extern "C" kmip_status_t kmip_rotary(const void* X, void* Y, int32_t H, const vo
     const int32_t si = size_of(dtype_in), so = size_of(dtype_out);
     const int64_t packed[8] = {(int64_t)H * d, d, (int64_t)H * d, d, (int64_t)H2 * d, d, (int64_t)H2 * d, d};
     const int64_t* st = strides != nullptr ? strides : packed;
-    // the widest runs of pairs that sizes, strides and pointers allow
-    int pairs = 8;
+    // the longest runs, up to 16 bytes, that sizes, strides and pointers allow
     auto fits = [&](int p) {
-        if (rot / 2 % p != 0 || (d - rot) % (2 * p) != 0) return false;
-        const int32_t bi = p * si < 16 ? p * si : 16, bo = p * so < 16 ? p * so : 16;
+        if (rot / 2 % p != 0 || (d - rot) % (2 * p) != 0 || p * si > 16 || p * so > 16) return false;
         for (int t = 0; t < (H2 > 0 ? 2 : 1); ++t) {
             const void *x = t ? X2 : X, *y = t ? Y2 : Y;
-            if (reinterpret_cast<uintptr_t>(x) % bi != 0 || reinterpret_cast<uintptr_t>(y) % bo != 0) return false;
-            for (int i = 0; i < 2; ++i)
-                if (st[4 * t + i] * si % bi != 0 || st[4 * t + 2 + i] * so % bo != 0) return false;
+            if (reinterpret_cast<uintptr_t>(x) % (p * si) != 0 || reinterpret_cast<uintptr_t>(y) % (p * so) != 0) return false;
+            for (int i = 0; i < 4; ++i)
+                if (st[4 * t + i] % p != 0) return false;
         }
         return true;
     };
-    if (!fits(8)) pairs = fits(4) ? 4 : 1;
+    const int pairs = fits(8) ? 8 : fits(4) ? 4 : 1;
     for (int t = 0; t < (H2 > 0 ? 2 : 1); ++t) {
         const void *x = t ? X2 : X, *y = t ? Y2 : Y;
         if (reinterpret_cast<uintptr_t>(x) % si != 0 || reinterpret_cast<uintptr_t>(y) % so != 0)
@@ -247,8 +266,12 @@ extern "C" kmip_status_t kmip_rotary(const void* X, void* Y, int32_t H, const vo
     a.threads = (uint32_t)threads;
     a.heads = H + H2;
     a.first_heads = H;
-    // Heads a thread takes: as many as leave 2^18 threads (16 waves a CU)
-    const int64_t groups = (int64_t(1) << 18) / threads + 1;
+    // Heads a thread takes: as many as leave 2^19 threads (32 waves a CU; 16,383
+    // tokens of 40 heads, d = 128, rot = 64: 75 us with 2^18, 73, 76 with 2^20)
+    const int64_t groups = (int64_t(1) << 19) / threads + 1;
+    // Results larger than the chip's 32 MB of L2 are stored past it (the same
+    // tokens 73 -> 68 us; 100,000 of 8 heads, d = 32, float32 to bf16 and back 75 -> 63)
+    a.pass_by = N * a.heads * d * so > (int64_t(32) << 20);
     a.group = groups >= a.heads ? 1 : (int32_t)((a.heads + groups - 1) / groups);
     int32_t ny = (a.heads + a.group - 1) / a.group;
     if (ny > 65535) a.group = (a.heads + 65534) / 65535, ny = (a.heads + a.group - 1) / a.group;
