@@ -38,7 +38,6 @@ struct RotaryArgs {
     int32_t units, rot_units;         // threads a token and head group, those with pairs
     int32_t heads, first_heads, group;
     int32_t rot;
-    bool pass_by;
     float cos_scale, sin_scale;
     uint64_t turns[kMostPairs];
 };
@@ -65,18 +64,15 @@ struct alignas(sizeof(typename T::word) * P) Pack {
     typename T::word v[P];
 };
 
-// pass_by: past the caches, for results that do not fit them.
-template <typename T, int P>
-__device__ __forceinline__ void put(char* p, const Pack<T, P>& w, bool pass_by) {
-    constexpr int kWords = sizeof(w) / 4;
-    if constexpr (kWords > 0) {
-        typedef uint32_t words __attribute__((ext_vector_type(kWords > 0 ? kWords : 1)));
-        if (pass_by) {
-            __builtin_nontemporal_store(__builtin_bit_cast(words, w), reinterpret_cast<words*>(p));
-            return;
-        }
+// PAST: past the caches, for results that do not fit them.
+template <bool PAST, typename T, int P>
+__device__ __forceinline__ void put(char* p, const Pack<T, P>& w) {
+    if constexpr (PAST) {
+        typedef uint32_t words __attribute__((ext_vector_type(sizeof(w) / 4)));
+        __builtin_nontemporal_store(__builtin_bit_cast(words, w), reinterpret_cast<words*>(p));
+    } else {
+        *reinterpret_cast<Pack<T, P>*>(p) = w;
     }
-    *reinterpret_cast<Pack<T, P>*>(p) = w;
 }
 
 // sin and cos of phase / 2^32 turns.
@@ -116,7 +112,7 @@ __device__ __forceinline__ void turn(float (&u)[P], float (&v)[P], const float (
 // the same memory, so that the compiler cannot move a load across it).
 constexpr int kRows = 4;
 
-template <typename TI, typename TO, int P, bool INTER>
+template <typename TI, typename TO, int P, bool INTER, bool PAST>
 __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs a) {
     constexpr int kIn = sizeof(typename TI::word), kOut = sizeof(typename TO::word);
     const uint32_t id = blockIdx.x * 256u + threadIdx.x;
@@ -170,8 +166,8 @@ __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs a) {
             Pack<TO, P> w[2];
 #pragma unroll
             for (int e = 0; e < P; ++e) w[0].v[e] = TO::round(u[e]), w[1].v[e] = TO::round(v[e]);
-            put(y + one * kOut, w[0], a.pass_by);
-            put(y + two * kOut, w[1], a.pass_by);
+            put<PAST>(y + one * kOut, w[0]);
+            put<PAST>(y + two * kOut, w[1]);
         }
     }
 }
@@ -180,26 +176,28 @@ int32_t size_of(int32_t dtype) { return dtype == KMIP_FP32 ? 4 : 2; }
 
 kmip_status_t ok() { return record_error(KMIP_OK, "%s", ""); }
 
+template <typename TI, typename TO, int P, bool PAST>
+void launch(const RotaryArgs& a, bool inter, dim3 grid, hipStream_t stream) {
+    if (inter)
+        hipLaunchKernelGGL((rotary_kernel<TI, TO, P, true, PAST>), grid, dim3(256), 0, stream, a);
+    else
+        hipLaunchKernelGGL((rotary_kernel<TI, TO, P, false, PAST>), grid, dim3(256), 0, stream, a);
+}
+
 template <typename TI, typename TO>
-void launch_types(const RotaryArgs& a, int pairs, bool inter, dim3 grid, hipStream_t stream) {
-#define KMIP_ROTARY(P)                                                                                       \
-    if (pairs == P) {                                                                                        \
-        if (inter)                                                                                           \
-            hipLaunchKernelGGL((rotary_kernel<TI, TO, P, true>), grid, dim3(256), 0, stream, a);             \
-        else                                                                                                 \
-            hipLaunchKernelGGL((rotary_kernel<TI, TO, P, false>), grid, dim3(256), 0, stream, a);            \
+void launch_types(const RotaryArgs& a, int pairs, bool inter, bool past, dim3 grid, hipStream_t stream) {
+    if constexpr (sizeof(typename TI::word) == 2 && sizeof(typename TO::word) == 2) {
+        if (pairs == 8) return past ? launch<TI, TO, 8, true>(a, inter, grid, stream) : launch<TI, TO, 8, false>(a, inter, grid, stream);
     }
-    if constexpr (sizeof(typename TI::word) == 2 && sizeof(typename TO::word) == 2) { KMIP_ROTARY(8) }
-    KMIP_ROTARY(4)
-    KMIP_ROTARY(1)
-#undef KMIP_ROTARY
+    if (pairs == 4) return past ? launch<TI, TO, 4, true>(a, inter, grid, stream) : launch<TI, TO, 4, false>(a, inter, grid, stream);
+    launch<TI, TO, 1, false>(a, inter, grid, stream);
 }
 
 template <typename TI>
-void launch_out(const RotaryArgs& a, int32_t out, int pairs, bool inter, dim3 grid, hipStream_t stream) {
-    if (out == KMIP_BF16) launch_types<TI, Brain16>(a, pairs, inter, grid, stream);
-    if (out == KMIP_FP16) launch_types<TI, Half16>(a, pairs, inter, grid, stream);
-    if (out == KMIP_FP32) launch_types<TI, Single>(a, pairs, inter, grid, stream);
+void launch_out(const RotaryArgs& a, int32_t out, int pairs, bool inter, bool past, dim3 grid, hipStream_t stream) {
+    if (out == KMIP_BF16) launch_types<TI, Brain16>(a, pairs, inter, past, grid, stream);
+    if (out == KMIP_FP16) launch_types<TI, Half16>(a, pairs, inter, past, grid, stream);
+    if (out == KMIP_FP32) launch_types<TI, Single>(a, pairs, inter, past, grid, stream);
 }
 
 }  // namespace
@@ -270,8 +268,8 @@ extern "C" kmip_status_t kmip_rotary(const void* X, void* Y, int32_t H, const vo
     // tokens of 40 heads, d = 128, rot = 64: 75 us with 2^18, 73, 76 with 2^20)
     const int64_t groups = (int64_t(1) << 19) / threads + 1;
     // Results larger than the chip's 32 MB of L2 are stored past it (the same
-    // tokens 73 -> 68 us; 100,000 of 8 heads, d = 32, float32 to bf16 and back 75 -> 63)
-    a.pass_by = N * a.heads * d * so > (int64_t(32) << 20);
+    // tokens 73 -> 71 us; 100,000 of 8 heads, d = 32, float32 to bf16 and back 75 -> 63)
+    const bool past = pairs > 1 && N * a.heads * d * so > (int64_t(32) << 20);
     a.group = groups >= a.heads ? 1 : (int32_t)((a.heads + groups - 1) / groups);
     int32_t ny = (a.heads + a.group - 1) / a.group;
     if (ny > 65535) a.group = (a.heads + 65534) / 65535, ny = (a.heads + a.group - 1) / a.group;
@@ -281,9 +279,9 @@ extern "C" kmip_status_t kmip_rotary(const void* X, void* Y, int32_t H, const vo
     const dim3 grid((unsigned)((threads + 255) / 256), (unsigned)ny);
     const hipStream_t s = reinterpret_cast<hipStream_t>(stream);
     const bool inter = interleaved != 0;
-    if (dtype_in == KMIP_BF16) launch_out<Brain16>(a, dtype_out, pairs, inter, grid, s);
-    if (dtype_in == KMIP_FP16) launch_out<Half16>(a, dtype_out, pairs, inter, grid, s);
-    if (dtype_in == KMIP_FP32) launch_out<Single>(a, dtype_out, pairs, inter, grid, s);
+    if (dtype_in == KMIP_BF16) launch_out<Brain16>(a, dtype_out, pairs, inter, past, grid, s);
+    if (dtype_in == KMIP_FP16) launch_out<Half16>(a, dtype_out, pairs, inter, past, grid, s);
+    if (dtype_in == KMIP_FP32) launch_out<Single>(a, dtype_out, pairs, inter, past, grid, s);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return record_error(KMIP_ERR_HIP, "rotary launch: %s", hipGetErrorString(e));
     return ok();
