@@ -121,12 +121,15 @@ kmip_status_t cut(std::vector<Seq>& seqs, bool causal, const Tiles& tiles_of, co
         l.tile_jobs = (int32_t)tile_jobs;
         l.first_job = (int32_t)p->jobs;
         // two workgroups a CU are resident at once (see full_tile)
-        l.fold = causal && jobs <= 512;
+        l.fold = p->halves == 1 && causal && jobs <= 512;
         p->jobs += jobs;
     }
     return KMIP_OK;
 }
 
+#ifndef HALFMIN
+#define HALFMIN 1024
+#endif
 constexpr int64_t kSlots = 512;   // workgroups resident at once, two on each of 256 CUs
 
 int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
@@ -137,9 +140,10 @@ int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 //     tiles that are at least half full and fill the chip, by themselves or in runs
 //     of at least 512 streamed rows.
 //   32 rows otherwise, in runs of at least 512 where that makes more jobs.
+// Two groups of four waves share a tile (halves) ... `wide`: the kernel for keys at D = 128 has this form only.
 // Runs cost the sums' way through memory, so that there are as few as fill the chip.
 template <typename Kept, typename Streamed>
-kmip_status_t plan(std::vector<Seq>& seqs, int32_t Hk, bool causal, const Kept& kept_of, const Streamed& streamed_of, FullPlan* p) {
+kmip_status_t plan(std::vector<Seq>& seqs, int32_t Hk, bool causal, const Kept& kept_of, const Streamed& streamed_of, bool wide, FullPlan* p) {
     auto tiles = [&](const Seq& s, int64_t rows) { return (kept_of(s) + rows - 1) / rows * Hk; };
     int64_t kept = 0, jobs = 0, work = 0, work32 = 0, longest = 0;
     for (const Seq& s : seqs) {
@@ -151,6 +155,7 @@ kmip_status_t plan(std::vector<Seq>& seqs, int32_t Hk, bool causal, const Kept& 
     }
     const bool full = 2 * kept >= 128 * jobs;
     p->rows = full && (jobs >= kSlots || work >= kSlots * 512) ? 128 : 32;
+    p->halves = p->rows == 128 && (wide || work >= jobs * HALFMIN) ? 2 : 1;
     int64_t run = 0;
     if (p->rows == 32)
         run = std::max<int64_t>(round_up(work32 / (2 * kSlots), 128), 512);
@@ -166,16 +171,16 @@ kmip_status_t plan_rows(const Sequences& sq, int32_t H, int32_t Hk, bool causal,
     std::vector<Seq> seqs;
     for (int32_t g = 0; g < sq.count; ++g)
         if (sq.at(g).q_len > 0) seqs.push_back(sq.at(g));
-    return plan(seqs, Hk, causal, [=](const Seq& s) { return s.q_len * rep; }, [](const Seq& s) { return (int64_t)s.k_len; }, p);
+    return plan(seqs, Hk, causal, [=](const Seq& s) { return s.q_len * rep; }, [](const Seq& s) { return (int64_t)s.k_len; }, false, p);
 }
 
 // Key tiles cover every slot, since rows without a gradient are written too.
-kmip_status_t plan_keys(const Sequences& sq, int32_t H, int32_t Hk, bool causal, FullPlan* p) {
+kmip_status_t plan_keys(const Sequences& sq, int32_t H, int32_t Hk, bool causal, bool wide, FullPlan* p) {
     const int64_t rep = H / Hk;
     std::vector<Seq> seqs;
     for (int32_t g = 0; g < sq.count; ++g)
         if (sq.at(g).k_slot > 0) seqs.push_back(sq.at(g));
-    return plan(seqs, Hk, causal, [](const Seq& s) { return (int64_t)s.k_slot; }, [=](const Seq& s) { return s.q_len * rep; }, p);
+    return plan(seqs, Hk, causal, [](const Seq& s) { return (int64_t)s.k_slot; }, [=](const Seq& s) { return s.q_len * rep; }, wide, p);
 }
 
 // Workspace of the forward: the runs' sums, then their maxima and sums of weights.
@@ -308,7 +313,7 @@ size_t kmip_full_bwd_workspace_size(const int32_t* q_offsets, const int32_t* k_o
         FullPlan dq, dkv;
         kmip_status_t e = check_call(q_offsets, k_offsets, k_lengths, num_seqs, Nq, Nk, H, Hk, d, dv, &sq);
         if (e == KMIP_OK) e = plan_rows(sq, H, Hk, false, &dq);
-        if (e == KMIP_OK) e = plan_keys(sq, H, Hk, false, &dkv);
+        if (e == KMIP_OK) e = plan_keys(sq, H, Hk, false, std::max(d, dv) == 128, &dkv);
         if (e == KMIP_OK) bytes = bwd_layout(dq, dkv, Nq, H, d, dv).total;
         return e;
     });
@@ -335,7 +340,7 @@ kmip_status_t kmip_full_bwd(const void* Q, const void* K, const void* V, const v
             if (e == KMIP_OK && (reinterpret_cast<uintptr_t>(p) & 15u) != 0)
                 e = record_error(KMIP_ERR_INVALID_ARG, "out, dQ, dK and dV must be 16-byte aligned");
         if (e == KMIP_OK) e = plan_rows(sq, H, Hk, causal != 0, &dq);
-        if (e == KMIP_OK) e = plan_keys(sq, H, Hk, causal != 0, &dkv);
+        if (e == KMIP_OK) e = plan_keys(sq, H, Hk, causal != 0, std::max(d, dv) == 128, &dkv);
         if (e != KMIP_OK) return e;
         const BwdLayout L = bwd_layout(dq, dkv, Nq, H, d, dv);
         if ((e = check_workspace(workspace, workspace_bytes, L.total)) != KMIP_OK) return e;

@@ -12,6 +12,8 @@
 //                    other of its group: s, dp, then dv and dk.
 // They form s and dp twice, seven products where one pass with atomics would
 // need five.  Forms for many and for few kept rows as in the forward.
+#include <type_traits>
+
 #include "full_common.h"
 
 namespace kmip {
@@ -32,16 +34,17 @@ struct BwdArgs {
     FullSeqs s;
 };
 
-template <typename T, int D, int ROWS>
-__global__ __launch_bounds__(256, ROWS == 128 ? 2 : 1) void full_dq_kernel(const BwdArgs a) {
+template <typename T, int D, int ROWS, int HALVES>
+__global__ __launch_bounds__(256 * HALVES, ROWS == 128 ? 2 : 1) void full_dq_kernel(const BwdArgs a) {
     constexpr int kTile = ROWS == 128 ? (D == 16 ? 128 : 64) : 32;
     constexpr int kBytes = kTile * 2 * D;
-    constexpr int kWaves = 4, kOwn = ROWS == 128 ? 1 : kWaves;
+    constexpr int kWaves = 4, kOwn = ROWS == 128 ? HALVES : kWaves;
     constexpr int kBufs = ROWS == 128 ? 2 : kStages<D>;
     constexpr int kT = D < 32 ? 1 : D / 32;
     __shared__ __attribute__((aligned(1024))) char sh[kOwn * kBufs * 2 * kBytes];
 
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6 & 3);
+    const int half = HALVES > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 8) : 0;
     const RowJob j = row_job<ROWS>(a.s, a.Hk, a.rep, a.causal, a.fold, a.split, blockIdx.x, lane);
     const int32_t nrows = j.q_len * a.rep;
     const int32_t row0 = j.tile * ROWS + (ROWS == 128 ? 32 * wave : 0);
@@ -72,19 +75,19 @@ __global__ __launch_bounds__(256, ROWS == 128 ? 2 : 1) void full_dq_kernel(const
     const float lse = a.lse[at];
     // a row that sees no key: every weight 0
     const float lse2 = lse == -INFINITY ? INFINITY : lse * kLog2e;
-    if (live && lane < 32 && (ROWS == 128 || wave == 0) && j.run == 0) {
+    if (live && lane < 32 && (ROWS == 128 ? half == 0 : wave == 0) && j.run == 0) {
         a.lse2[at] = lse2;
         a.D[at] = di;
     }
     const float c = a.scale * kLog2e;
-    const int32_t lim = sees(row), lim_first = sees(row0), lim_last = sees(row0 + 31);
+    const int32_t lim = sees(row), lim_first = sees(row0), lim_last = row0 < nrows ? sees(row0 + 31) : 0;
     const int32_t lo = a.split > 0 ? j.run * a.split : 0;
     int32_t hi = sees(j.tile * ROWS + ROWS - 1);
     if (j.runs > 1) hi = min(hi, lo + a.split);
 
     const char* kp = a.k + (int64_t)j.k_lo * a.k_row + j.kv_head * a.k_head;
     const char* vp = a.v + (int64_t)j.k_lo * a.v_row + j.kv_head * a.v_head;
-    const uint32_t base = lds_addr(sh) + (ROWS == 128 ? 0 : wave * kBufs * 2 * kBytes);
+    const uint32_t base = lds_addr(sh) + (ROWS == 128 ? half : wave) * kBufs * 2 * kBytes;
     constexpr int kParts = ROWS == 128 ? kWaves : 1;
     const int part = ROWS == 128 ? wave : 0;
     TileLoad<D, kParts> kl, vl;
@@ -97,20 +100,18 @@ __global__ __launch_bounds__(256, ROWS == 128 ? 2 : 1) void full_dq_kernel(const
     f32x16 acc[kT];
 #pragma unroll
     for (int t = 0; t < kT; ++t) clear(acc[t]);
-    auto compute = [&](int32_t key0, int buf) {
-        const uint32_t kt = base + buf * 2 * kBytes;
-        const uint32_t ka = row_operand<D>(kt, lane), va = row_operand<D>(kt + kBytes, lane);
-        uint32_t ta[2];
-        tr_operand<D>(ta, kt, lane);
+    Operands<D> in;
+    in.init(base, lane);
+    auto compute = [&](int32_t key0, auto k_at, auto v_at) {
 #pragma unroll
         for (int b = 0; b < kTile / 32; ++b) {
             f32x16 s, dp;
             clear(s);
             clear(dp);
 #pragma unroll
-            for (int t = 0; t < D / 16; ++t) s = T::mfma(lds_row16((ka ^ (32 * t)) + b * 64 * D), q[t], s);
+            for (int t = 0; t < D / 16; ++t) s = T::mfma(in.rows(t, k_at + b * 64 * D), q[t], s);
 #pragma unroll
-            for (int t = 0; t < D / 16; ++t) dp = T::mfma(lds_row16((va ^ (32 * t)) + b * 64 * D), g[t], dp);
+            for (int t = 0; t < D / 16; ++t) dp = T::mfma(in.rows(t, v_at + b * 64 * D), g[t], dp);
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], c, -lse2)) * (dp[r] - di);
             if (key0 + 32 * b + 32 > lim_first) {
@@ -123,21 +124,27 @@ __global__ __launch_bounds__(256, ROWS == 128 ? 2 : 1) void full_dq_kernel(const
             for (int i = 0; i < 2; ++i) {
                 const s16x8 p = round8<T>(s, i);   // rounded to the inputs' type, the operand of the product
 #pragma unroll
-                for (int t = 0; t < kT; ++t) {
-                    const uint32_t o = (32 * b + 16 * i) * 2 * D;
-                    acc[t] = T::mfma(lds_rows_tr((ta[0] ^ (64 * t)) + o, (ta[1] ^ (64 * t)) + o), p, acc[t]);
-                }
+                for (int t = 0; t < kT; ++t) acc[t] = T::mfma(in.columns(t, k_at + (32 * b + 16 * i) * 2 * D), p, acc[t]);
             }
         }
     };
     if constexpr (ROWS == 128) {
-        if (lo < hi) fetch(lo, 0);
-        int buf = 0;
-        for (int32_t key = lo; key < hi; key += kTile, buf ^= 1) {
+        const int32_t n = lo < hi ? (hi - lo - 1) / kTile + 1 : 0, most = (n + HALVES - 1) / HALVES;
+        const int32_t first = lo + half * most * kTile, mine = half == 0 ? most : n - most;
+        if (mine > 0) fetch(first, 0);
+        auto stage = [&](int32_t i, auto buf) {
+            const int32_t key = first + i * kTile;
             wait_and_sync();
-            if (key + kTile < hi) fetch(key + kTile, buf ^ 1);
-            if (key < lim_last) compute(key, buf);
+            if (i + 1 < mine) fetch(key + kTile, buf ^ 1);
+            if (i < mine && key < lim_last)
+                compute(key, Constant<decltype(buf)::value * 2 * kBytes>(), Constant<decltype(buf)::value * 2 * kBytes + kBytes>());
+        };
+        for (int32_t i = 0; i < most; i += 2) {
+            stage(i, std::integral_constant<int, 0>());
+            if (i + 1 < most) stage(i + 1, std::integral_constant<int, 1>());
         }
+        if constexpr (HALVES > 1)
+            if (!add_half<kT>(acc, sh, wave, half, lane)) return;
         if (!live) return;
         const int64_t job = (int64_t)a.first_job + blockIdx.x;
 #pragma unroll
@@ -152,7 +159,10 @@ __global__ __launch_bounds__(256, ROWS == 128 ? 2 : 1) void full_dq_kernel(const
         const int32_t mine = lo + 32 * wave, n = mine < hi ? (hi - mine + 32 * kWaves - 1) / (32 * kWaves) : 0;
         stream_blocks<kBufs, 2 * kTile / TileLoad<D, 1>::kPer>(
             n, [&](int32_t i, int stage) { fetch(mine + 32 * kWaves * i, stage); },
-            [&](int32_t i, int stage) { compute(mine + 32 * kWaves * i, stage); });
+            [&](int32_t i, int stage) {
+                const uint32_t at = stage * 2 * kBytes;
+                compute(mine + 32 * kWaves * i, at, at + kBytes);
+            });
         // the four waves' sums, in their order
         wait_and_sync();
         float* const so = reinterpret_cast<float*>(sh);
@@ -175,19 +185,22 @@ __global__ __launch_bounds__(256, ROWS == 128 ? 2 : 1) void full_dq_kernel(const
     }
 }
 
-template <typename T, int D, int KEYS>
-__global__ __launch_bounds__(256, KEYS == 128 ? 2 : 1) void full_dkv_kernel(const BwdArgs a) {
+template <typename T, int D, int KEYS, int HALVES>
+__global__ __launch_bounds__(256 * HALVES, KEYS == 128 ? 2 : 1) void full_dkv_kernel(const BwdArgs a) {
     constexpr int kTile = KEYS == 128 ? (D == 16 ? 128 : D == 128 ? 32 : 64) : 32;   // tokens a buffer holds
-    constexpr bool kHeld = KEYS == 32 || D < 128;   // V in registers, else in LDS
+    // The kept K and V stay in registers, or are read from LDS where registers would spill
+    constexpr int kSteps = D / 16;
+    constexpr bool kHeld = KEYS == 32 || D < 128;
     constexpr int kBytes = kTile * 2 * D;
-    constexpr int kWaves = 4, kOwn = KEYS == 128 ? 1 : kWaves;
+    constexpr int kWaves = 4, kOwn = KEYS == 128 ? HALVES : kWaves;
     constexpr int kBufs = KEYS == 128 ? 2 : kStages<D>;
     constexpr int kT = D < 32 ? 1 : D / 32;
     __shared__ __attribute__((aligned(1024))) char sh[kOwn * kBufs * 2 * kBytes];   // [buffer][Q, dout]
-    __shared__ __attribute__((aligned(1024))) char shv[kHeld ? 1024 : KEYS * 2 * D];   // V of the kept keys
+    __shared__ __attribute__((aligned(1024))) s16x8 kept[kHeld ? 1 : kWaves * 2 * kSteps * 64];   // [wave][K's, V's][lane]
     __shared__ __attribute__((aligned(16))) float st[kOwn][kBufs][2][kTile];   // [buffer][lse log2 e, D]
 
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6 & 3);
+    const int half = HALVES > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 8) : 0;
     const int sq = __builtin_amdgcn_readfirstlane(seq_of_job(a.s, blockIdx.x, lane));
     const int32_t q_lo = a.s.q_lo[sq], q_len = a.s.q_len[sq], k_lo = a.s.k_lo[sq], k_len = a.s.k_len[sq], slot = a.s.k_slot[sq];
     const int32_t runs = full_runs((int64_t)q_len * a.rep, a.split), kv_head = (blockIdx.x - a.s.job0[sq]) % a.Hk;
@@ -197,17 +210,18 @@ __global__ __launch_bounds__(256, KEYS == 128 ? 2 : 1) void full_dkv_kernel(cons
     const int32_t tile_lo = tile * KEYS;                       // keys from here on
     const int32_t key0 = tile_lo + (KEYS == 128 ? 32 * wave : 0), key = key0 + (lane & 31);
     const int64_t key_at = min(key, max(k_len, 1) - 1);
-    s16x8 k[D / 16], v[kHeld ? D / 16 : 1];
+    s16x8 k[D / 16], v[D / 16];
     if (k_len > 0) {
         load_columns<D>(k, a.k + (k_lo + key_at) * a.k_row + kv_head * a.k_head, a.d, lane);
-        if constexpr (kHeld) load_columns<D>(v, a.v + (k_lo + key_at) * a.v_row + kv_head * a.v_head, a.dv, lane);
+        load_columns<D>(v, a.v + (k_lo + key_at) * a.v_row + kv_head * a.v_head, a.dv, lane);
     } else {
 #pragma unroll
-        for (int t = 0; t < D / 16; ++t) k[t] = s16x8{};
-        if constexpr (kHeld) {
+        for (int t = 0; t < D / 16; ++t) k[t] = v[t] = s16x8{};
+    }
+    s16x8* const own = kept + (kHeld ? 0 : wave * 2 * kSteps * 64 + lane);   // (both halves')
+    if (!kHeld && half == 0) {
 #pragma unroll
-            for (int t = 0; t < D / 16; ++t) v[t] = s16x8{};
-        }
+        for (int t = 0; t < kSteps; ++t) own[t * 64] = k[t], own[(kSteps + t) * 64] = v[t];
     }
     // the first token that sees the tile, and its first and last key of this wave
     const int32_t t_lo = tile_lo >= k_len ? q_len : a.causal ? max(0, tile_lo - off) : 0;
@@ -217,8 +231,8 @@ __global__ __launch_bounds__(256, KEYS == 128 ? 2 : 1) void full_dkv_kernel(cons
     f32x16 dk[kT], dv[kT];
 #pragma unroll
     for (int t = 0; t < kT; ++t) clear(dk[t]), clear(dv[t]);
-    const uint32_t base = lds_addr(sh) + (KEYS == 128 ? 0 : wave * kBufs * 2 * kBytes);
-    float(*const stats)[2][kTile] = st[KEYS == 128 ? 0 : wave];
+    const uint32_t base = lds_addr(sh) + (KEYS == 128 ? half : wave) * kBufs * 2 * kBytes;
+    float(*const stats)[2][kTile] = st[KEYS == 128 ? half : wave];
     constexpr int kParts = KEYS == 128 ? kWaves : 1;
     const int part = KEYS == 128 ? wave : 0;
     TileLoad<D, kParts> ql, gl;
@@ -238,49 +252,48 @@ __global__ __launch_bounds__(256, KEYS == 128 ? 2 : 1) void full_dkv_kernel(cons
             load_word_to_lds(st_base + buf * kTile * 8 + 256 * part, (i < kTile ? a.lse2 : a.D) + at);
         }
     };
-    const uint32_t kept_v = kHeld ? 0 : row_operand<D>(lds_addr(shv) + wave * 64 * D, lane);
-    auto compute = [&](int32_t tok, int buf) {
-        const uint32_t qt = base + buf * 2 * kBytes;
-        const uint32_t qa = row_operand<D>(qt, lane), ga = row_operand<D>(qt + kBytes, lane);
-        uint32_t tq[2], tg[2];
-        tr_operand<D>(tq, qt, lane);
-        tr_operand<D>(tg, qt + kBytes, lane);
+    Operands<D> in;
+    in.init(base, lane);
+    auto compute = [&](int32_t tok, auto q_at, auto g_at, int buf) {
 #pragma unroll
         for (int b = 0; b < kTile / 32; ++b) {
             f32x16 s, dp;
             clear(s);
             clear(dp);
 #pragma unroll
-            for (int t = 0; t < D / 16; ++t) s = T::mfma(lds_row16((qa ^ (32 * t)) + b * 64 * D), k[t], s);
+            for (int t = 0; t < D / 16; ++t) s = T::mfma(in.rows(t, q_at + b * 64 * D), kHeld ? k[t] : own[t * 64], s);
 #pragma unroll
-            for (int t = 0; t < D / 16; ++t) {
-                if (!kHeld && 16 * t >= a.dv) break;   // (neither side has zeros there)
-                dp = T::mfma(lds_row16((ga ^ (32 * t)) + b * 64 * D), kHeld ? v[kHeld ? t : 0] : lds_row16(kept_v ^ (32 * t)), dp);
-            }
+            for (int t = 0; t < D / 16; ++t)
+                dp = T::mfma(in.rows(t, g_at + b * 64 * D), kHeld ? v[t] : own[(kSteps + t) * 64], dp);
             const float* sb = &stats[buf][0][32 * b + 4 * (lane >> 5)];
-            // rows of the block that see the key; those behind the last token do not
-            const bool edge = tok + 32 * b < t_all || tok + 32 * b + 32 > q_len;
-            const int32_t from = a.causal ? key - off - tok - 32 * b - 4 * (lane >> 5) : 0, upto = q_len - tok - 32 * b - 4 * (lane >> 5);
 #pragma unroll
             for (int r = 0; r < 16; r += 4) {
-                const f32x4 l = *reinterpret_cast<const f32x4*>(sb + 2 * r), di = *reinterpret_cast<const f32x4*>(sb + kTile + 2 * r);
+                const f32x4 l = *reinterpret_cast<const f32x4*>(sb + 2 * r);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float p = __builtin_amdgcn_exp2f(fmaf(s[r + e], c, -l[e]));
-                    float x = p * (dp[r + e] - di[e]);
-                    if (edge && (e + 2 * r < from || e + 2 * r >= upto)) p = 0.0f, x = 0.0f;
-                    s[r + e] = p;
-                    dp[r + e] = x;
+                for (int e = 0; e < 4; ++e) s[r + e] = __builtin_amdgcn_exp2f(fmaf(s[r + e], c, -l[e]));
+            }
+            // rows of the block that do not see the key, or lie behind the last token
+            if (tok + 32 * b < t_all || tok + 32 * b + 32 > q_len) {
+                const int32_t from = a.causal ? key - off - tok - 32 * b - 4 * (lane >> 5) : 0, upto = q_len - tok - 32 * b - 4 * (lane >> 5);
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int i = (r & 3) + 8 * (r >> 2);
+                    if (i < from || i >= upto) s[r] = 0.0f;
                 }
+            }
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+                const f32x4 di = *reinterpret_cast<const f32x4*>(sb + kTile + 2 * r);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) dp[r + e] = s[r + e] * (dp[r + e] - di[e]);
             }
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const s16x8 p = round8<T>(s, i), x = round8<T>(dp, i);   // rounded, the operands of the products
 #pragma unroll
                 for (int t = 0; t < kT; ++t) {
-                    const uint32_t o = (32 * b + 16 * i) * 2 * D;
-                    dv[t] = T::mfma(lds_rows_tr((tg[0] ^ (64 * t)) + o, (tg[1] ^ (64 * t)) + o), p, dv[t]);
-                    dk[t] = T::mfma(lds_rows_tr((tq[0] ^ (64 * t)) + o, (tq[1] ^ (64 * t)) + o), x, dk[t]);
+                    dv[t] = T::mfma(in.columns(t, g_at + (32 * b + 16 * i) * 2 * D), p, dv[t]);
+                    dk[t] = T::mfma(in.columns(t, q_at + (32 * b + 16 * i) * 2 * D), x, dk[t]);
                 }
             }
         }
@@ -291,30 +304,32 @@ __global__ __launch_bounds__(256, KEYS == 128 ? 2 : 1) void full_dkv_kernel(cons
     const int64_t all = t_lo < q_len ? (int64_t)per * a.rep : 0;
     const int32_t first = (int32_t)(all * run / runs), n = (int32_t)(all * (run + 1) / runs) - first;
     const int64_t job = (int64_t)a.first_job + blockIdx.x;
-    if constexpr (!kHeld) {
-        if (n > 0) {
-            TileLoad<D, kWaves> vl;
-            vl.init(lane, wave, a.dv, (uint32_t)a.v_row);
-            vl.template issue<KEYS>(lds_addr(shv), a.v + (k_lo + (int64_t)tile_lo) * a.v_row + kv_head * a.v_head, wave, k_len - tile_lo);
-        }
-    }
     if constexpr (KEYS == 128) {
-        int32_t hr = 0, tok = 0;
-        if (n > 0) {
-            hr = first / per;
-            tok = t_lo + first % per * kTile;
+        const int32_t most = (n + HALVES - 1) / HALVES, mine = half == 0 ? most : n - most, begin = first + half * most;
+        int32_t hr = 0, tok = 0;   // of the tile that is fetched next
+        if (mine > 0) {
+            hr = begin / per;
+            tok = t_lo + begin % per * kTile;
             fetch(hr, tok, 0);
         }
-        for (int32_t i = 0; i < n; ++i) {
-            const int buf = i & 1;
+        auto stage = [&](int32_t i, auto buf) {
             const int32_t now = tok;
             wait_and_sync();
-            if (i + 1 < n) {
+            if (i + 1 < mine) {
                 tok += kTile;
                 if (tok >= q_len) tok = t_lo, ++hr;
                 fetch(hr, tok, buf ^ 1);
             }
-            if (now + kTile > t_wave) compute(now, buf);
+            if (i < mine && now + kTile > t_wave)
+                compute(now, Constant<decltype(buf)::value * 2 * kBytes>(), Constant<decltype(buf)::value * 2 * kBytes + kBytes>(), decltype(buf)::value);
+        };
+        for (int32_t i = 0; i < most; i += 2) {
+            stage(i, std::integral_constant<int, 0>());
+            if (i + 1 < most) stage(i + 1, std::integral_constant<int, 1>());
+        }
+        if constexpr (HALVES > 1) {
+            add_half<kT>(dk, sh, wave, half, lane);
+            if (!add_half<kT>(dv, sh, wave, half, lane)) return;
         }
         if (key >= slot) return;
         const int64_t at = (k_lo + (int64_t)key) * a.Hk + kv_head;
@@ -337,7 +352,10 @@ __global__ __launch_bounds__(256, KEYS == 128 ? 2 : 1) void full_dkv_kernel(cons
         auto tok_of = [&](int32_t i) { return t_lo + (first + wave + kWaves * i) % per * kTile; };
         stream_blocks<kBufs, 2 * kTile / TileLoad<D, 1>::kPer + 1>(
             mine, [&](int32_t i, int stage) { fetch((first + wave + kWaves * i) / per, tok_of(i), stage); },
-            [&](int32_t i, int stage) { compute(tok_of(i), stage); });
+            [&](int32_t i, int stage) {
+                const uint32_t at = stage * 2 * kBytes;
+                compute(tok_of(i), at, at + kBytes, stage);
+            });
         // the four waves' sums, in their order: dK, then dV
         float* const so = reinterpret_cast<float*>(sh);
 #pragma unroll
@@ -432,20 +450,24 @@ hipError_t launch_bwd(const FullCall& f, const FullPlan& dq, const FullPlan& dkv
     a.scale = f.scale;
     for (const FullLaunch& l : dq.launches) {
         a.s = l.seqs, a.first_job = l.first_job, a.fold = l.fold, a.split = dq.split;
-        if (dq.rows == 128)
-            hipLaunchKernelGGL((full_dq_kernel<T, D, 128>), dim3(l.jobs), dim3(256), 0, stream, a);
+        if (dq.rows == 128 && dq.halves == 2)
+            hipLaunchKernelGGL((full_dq_kernel<T, D, 128, 2>), dim3(l.jobs), dim3(512), 0, stream, a);
+        else if (dq.rows == 128)
+            hipLaunchKernelGGL((full_dq_kernel<T, D, 128, 1>), dim3(l.jobs), dim3(256), 0, stream, a);
         else
-            hipLaunchKernelGGL((full_dq_kernel<T, D, 32>), dim3(l.jobs), dim3(256), 0, stream, a);
+            hipLaunchKernelGGL((full_dq_kernel<T, D, 32, 1>), dim3(l.jobs), dim3(256), 0, stream, a);
         hipError_t e = hipGetLastError();
         if (e == hipSuccess && l.tile_jobs > 0) e = launch_sum<T>(a, l, dq, ws.dq, a.dq, f.d, false, f.scale, stream);
         if (e != hipSuccess) return e;
     }
     for (const FullLaunch& l : dkv.launches) {
         a.s = l.seqs, a.first_job = l.first_job, a.fold = l.fold, a.split = dkv.split;
-        if (dkv.rows == 128)
-            hipLaunchKernelGGL((full_dkv_kernel<T, D, 128>), dim3(l.jobs), dim3(256), 0, stream, a);
+        if (dkv.rows == 128 && dkv.halves == 2)
+            hipLaunchKernelGGL((full_dkv_kernel<T, D, 128, 2>), dim3(l.jobs), dim3(512), 0, stream, a);
+        else if (dkv.rows == 128)
+            hipLaunchKernelGGL((full_dkv_kernel<T, D, 128, D == 128 ? 2 : 1>), dim3(l.jobs), dim3(256), 0, stream, a);
         else
-            hipLaunchKernelGGL((full_dkv_kernel<T, D, 32>), dim3(l.jobs), dim3(256), 0, stream, a);
+            hipLaunchKernelGGL((full_dkv_kernel<T, D, 32, 1>), dim3(l.jobs), dim3(256), 0, stream, a);
         hipError_t e = hipGetLastError();
         if (e == hipSuccess && l.tile_jobs > 0) e = launch_sum<T>(a, l, dkv, ws.dk, a.dk, f.d, true, f.scale, stream);
         if (e == hipSuccess && l.tile_jobs > 0) e = launch_sum<T>(a, l, dkv, ws.dv, a.dv_out, f.dv, true, 1.0f, stream);

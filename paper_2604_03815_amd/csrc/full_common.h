@@ -75,36 +75,47 @@ __device__ __forceinline__ uint32_t lds_addr(const void* p) {
     return (uint32_t)(uintptr_t)(const KMIP_LDS char*)p;
 }
 
-__device__ __forceinline__ s16x8 lds_row16(uint32_t a) { return *(const KMIP_LDS s16x8*)(uintptr_t)a; }
-
-__device__ __forceinline__ s16x8 lds_rows_tr(uint32_t a, uint32_t b) {
-    const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((KMIP_LDS s16x4*)(uintptr_t)a);
-    const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((KMIP_LDS s16x4*)(uintptr_t)b);
-    return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
-}
-
-// This lane's address of the plain left operand: rows R .. R + 31 (R a
-// multiple of 32) of a tile are at + R * 2D, dimensions 16 s .. 16 s + 15 at
-// ^ (32 s).
+// This lane's LDS addresses of the left operands in a tile at `tile`; a tile
+// elsewhere is at a distance, which becomes the instructions' offset where it is
+// known when compiling.
+//   row[t]: rows 0 .. 31, dimensions 16 t .. 16 t + 15; rows R .. R + 31 (R a multiple of 32) at + R * 2D;
+//   tr[i][t]: transposed, the tile's columns 32 t .. 32 t + 31 as operand rows and tile rows 0 .. 15
+//   as contraction, first and second half; rows R .. R + 15 (R a multiple of 16) at + R * 2D.
 template <int D>
-__device__ __forceinline__ uint32_t row_operand(uint32_t tile, int lane) {
-    const int r = lane & 31, c = lane >> 5;
-    return tile + r * 2 * D + ((c ^ swz<D>(r)) << 4);
-}
+struct Operands {
+    static constexpr int kT = D < 32 ? 1 : D / 32;
+    uint32_t row[D / 16], tr[2][kT];
 
-// This lane's addresses of the transposed left operand (columns 32 t .. 32 t +
-// 31 of the tile as operand rows, tile rows R .. R + 15, R a multiple of 16, as
-// contraction), first and second half: columns at ^ (64 t), rows at + R * 2D.
-template <int D>
-__device__ __forceinline__ void tr_operand(uint32_t (&a)[2], uint32_t tile, int lane) {
-    const int l = lane & 15, g = (lane >> 4) & 1, h = lane >> 5;
+    __device__ __forceinline__ void init(uint32_t tile, int lane) {
+        {
+            const int r = lane & 31, c = lane >> 5;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int r = 8 * i + 4 * h + (l >> 2);
-        const int c = (D >= 32 ? 2 * g : 0) + ((l >> 1) & 1);
-        a[i] = tile + r * 2 * D + ((c ^ swz<D>(r)) << 4) + (l & 1) * 8;
+            for (int t = 0; t < D / 16; ++t) row[t] = tile + r * 2 * D + (((c + 2 * t) ^ swz<D>(r)) << 4);
+        }
+        const int l = lane & 15, g = (lane >> 4) & 1, h = lane >> 5;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int r = 8 * i + 4 * h + (l >> 2);
+#pragma unroll
+            for (int t = 0; t < kT; ++t) {
+                const int c = 4 * t + (D >= 32 ? 2 * g : 0) + ((l >> 1) & 1);
+                tr[i][t] = tile + r * 2 * D + ((c ^ swz<D>(r)) << 4) + (l & 1) * 8;
+            }
+        }
     }
-}
+    __device__ __forceinline__ s16x8 rows(int t, uint32_t at) const { return *(const KMIP_LDS s16x8*)(uintptr_t)(row[t] + at); }
+    __device__ __forceinline__ s16x8 columns(int t, uint32_t at) const {
+        const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((KMIP_LDS s16x4*)(uintptr_t)(tr[0][t] + at));
+        const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((KMIP_LDS s16x4*)(uintptr_t)(tr[1][t] + at));
+        return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+};
+
+// A number known when compiling, for the buffers that alternate.
+template <uint32_t N>
+struct Constant {
+    __device__ constexpr operator uint32_t() const { return N; }
+};
 
 // x of this lane and of its partner lane ^ 32, as (lower lane's, upper lane's).
 __device__ __forceinline__ float2 both_halves(float x) {
@@ -324,6 +335,32 @@ __device__ __forceinline__ void put_piece(float* so, const f32x16& x, int t, flo
 template <int D>
 __device__ __forceinline__ f32x4 get_piece(const float* so, int row, int g) {
     return *reinterpret_cast<const f32x4*>(so + row * D + 4 * ((g ^ row) & (D / 4 - 1)));
+}
+
+// Adds the second half's sums of a tile to the first's through LDS (`sh`: 16 KB
+// per piece of 32 columns), for the first half; false for the second.  All
+// waves of the workgroup call it, when they are done with what sh holds.
+template <int KT>
+__device__ __forceinline__ bool add_half(f32x16 (&x)[KT], char* sh, int wave, int half, int lane) {
+    f32x4* const so = reinterpret_cast<f32x4*>(sh) + wave * KT * 256 + lane;
+    wait_and_sync();
+    if (half == 1) {
+#pragma unroll
+        for (int t = 0; t < KT; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) so[t * 256 + r * 16] = f32x4{x[t][r], x[t][r + 1], x[t][r + 2], x[t][r + 3]};
+    }
+    wait_and_sync();
+    if (half == 1) return false;
+#pragma unroll
+    for (int t = 0; t < KT; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+            const f32x4 y = so[t * 256 + r * 16];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[t][r + e] += y[e];
+        }
+    return true;
 }
 
 }  // namespace kmip

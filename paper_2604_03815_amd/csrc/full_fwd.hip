@@ -21,6 +21,8 @@
 //     end.  For few rows.
 // With `split` keys per job, jobs of a row tile take runs of its keys and write
 // partial sums, which full_join_kernel joins in the order of the runs.
+#include <type_traits>
+
 #include "full_common.h"
 
 namespace kmip {
@@ -48,16 +50,15 @@ struct FwdWave {
     float m, l;     // reference of the weights, sum of this lane's
     int32_t lim;    // keys this row sees
 
-    // NB blocks of 32 keys from key0 on.
-    template <int NB>
-    __device__ __forceinline__ void step(uint32_t ka, const uint32_t (&va)[2], int32_t key0, int32_t lim_first, float c,
-                                         int lane) {
+    // NB blocks of 32 keys from key0 on; keys and values at distances k_at and v_at.
+    template <int NB, typename KAt, typename VAt>
+    __device__ __forceinline__ void step(const Operands<D>& in, KAt k_at, VAt v_at, int32_t key0, int32_t lim_first, float c, int lane) {
         f32x16 s[NB];
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
             clear(s[b]);
 #pragma unroll
-            for (int t = 0; t < D / 16; ++t) s[b] = T::mfma(lds_row16((ka ^ (32 * t)) + b * 64 * D), q[t], s[b]);
+            for (int t = 0; t < D / 16; ++t) s[b] = T::mfma(in.rows(t, k_at + b * 64 * D), q[t], s[b]);
         }
         if (key0 + 32 * NB > lim_first) {
             const int32_t left = lim - key0 - 4 * (lane >> 5);
@@ -102,26 +103,24 @@ struct FwdWave {
                 // rounded to the inputs' type, the operand of the product: half a step of each weight
                 const s16x8 p = round8<T>(s[b], i);
 #pragma unroll
-                for (int t = 0; t < kT; ++t) {
-                    const uint32_t at = (32 * b + 16 * i) * 2 * D;
-                    o[t] = T::mfma(lds_rows_tr((va[0] ^ (64 * t)) + at, (va[1] ^ (64 * t)) + at), p, o[t]);
-                }
+                for (int t = 0; t < kT; ++t) o[t] = T::mfma(in.columns(t, v_at + (32 * b + 16 * i) * 2 * D), p, o[t]);
             }
         }
     }
 };
 
-template <typename T, int D, int ROWS>
-__global__ __launch_bounds__(256, ROWS == 128 ? 2 : 1) void full_fwd_kernel(const FwdArgs a) {
+template <typename T, int D, int ROWS, int HALVES>
+__global__ __launch_bounds__(256 * HALVES, ROWS == 128 ? 2 : 1) void full_fwd_kernel(const FwdArgs a) {
     constexpr int kTile = ROWS == 128 ? (D == 16 ? 128 : 64) : 32;   // keys a buffer holds
     constexpr int kBytes = kTile * 2 * D;                            // of one tensor's buffer
-    constexpr int kWaves = 4, kOwn = ROWS == 128 ? 1 : kWaves;       // buffer sets
+    constexpr int kWaves = 4, kOwn = ROWS == 128 ? HALVES : kWaves;  // buffer sets
     constexpr int kBufs = ROWS == 128 ? 2 : kStages<D>;
     constexpr int kT = FwdWave<T, D>::kT;
     __shared__ __attribute__((aligned(1024))) char sh[kOwn * kBufs * 2 * kBytes];
     static_assert(ROWS == 128 || sizeof(sh) >= 32 * D * 4 * kWaves, "room for the join");
 
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6 & 3);
+    const int half = HALVES > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 8) : 0;
     const RowJob j = row_job<ROWS>(a.s, a.Hk, a.rep, a.causal, a.fold, a.split, blockIdx.x, lane);
     const int32_t nrows = j.q_len * a.rep;
     const int32_t row0 = j.tile * ROWS + (ROWS == 128 ? 32 * wave : 0);
@@ -145,11 +144,11 @@ __global__ __launch_bounds__(256, ROWS == 128 ? 2 : 1) void full_fwd_kernel(cons
     const int32_t lo = a.split > 0 ? j.run * a.split : 0;
     int32_t hi = sees(j.tile * ROWS + ROWS - 1);
     if (a.split > 0) hi = min(hi, lo + a.split);
-    const int32_t lim_first = sees(row0), lim_last = sees(row0 + 31);
+    const int32_t lim_first = sees(row0), lim_last = row0 < nrows ? sees(row0 + 31) : 0;
     const float c = a.scale * kLog2e;
     const char* kp = a.k + (int64_t)j.k_lo * a.k_row + j.kv_head * a.k_head;
     const char* vp = a.v + (int64_t)j.k_lo * a.v_row + j.kv_head * a.v_head;
-    const uint32_t base = lds_addr(sh) + (ROWS == 128 ? 0 : wave * kBufs * 2 * kBytes);   // [buffer][K, V]
+    const uint32_t base = lds_addr(sh) + (ROWS == 128 ? half : wave) * kBufs * 2 * kBytes;   // [buffer][K, V]
     constexpr int kParts = ROWS == 128 ? kWaves : 1;
     const int part = ROWS == 128 ? wave : 0;
     TileLoad<D, kParts> kl, vl;
@@ -159,32 +158,68 @@ __global__ __launch_bounds__(256, ROWS == 128 ? 2 : 1) void full_fwd_kernel(cons
         kl.template issue<kTile>(base + buf * 2 * kBytes, kp + (int64_t)key * a.k_row, part, j.k_len - key);
         vl.template issue<kTile>(base + buf * 2 * kBytes + kBytes, vp + (int64_t)key * a.v_row, part, j.k_len - key);
     };
-    auto compute = [&](int32_t key, int buf) {
-        const uint32_t ka = row_operand<D>(base + buf * 2 * kBytes, lane);
-        uint32_t va[2];
-        tr_operand<D>(va, base + buf * 2 * kBytes + kBytes, lane);
-        w.template step<kTile / 32>(ka, va, key, lim_first, c, lane);
-    };
+    Operands<D> in;
+    in.init(base, lane);
     if constexpr (ROWS == 128) {
-        if (lo < hi) fetch(lo, 0);
-        int buf = 0;
-        for (int32_t key = lo; key < hi; key += kTile, buf ^= 1) {
+        // each half takes its part of the tiles; the first one's is as long or one longer
+        const int32_t n = lo < hi ? (hi - lo - 1) / kTile + 1 : 0, most = (n + HALVES - 1) / HALVES;
+        const int32_t first = lo + half * most * kTile, mine = half == 0 ? most : n - most;
+        if (mine > 0) fetch(first, 0);
+        auto stage = [&](int32_t i, auto buf) {
+            const int32_t key = first + i * kTile;
             wait_and_sync();
-            if (key + kTile < hi) fetch(key + kTile, buf ^ 1);
-            if (key < lim_last) compute(key, buf);
+            if (i + 1 < mine) fetch(key + kTile, buf ^ 1);
+            if (i < mine && key < lim_last)
+                w.template step<kTile / 32>(in, Constant<decltype(buf)::value * 2 * kBytes>(), Constant<decltype(buf)::value * 2 * kBytes + kBytes>(), key, lim_first, c, lane);
+        };
+        for (int32_t i = 0; i < most; i += 2) {
+            stage(i, std::integral_constant<int, 0>());
+            if (i + 1 < most) stage(i + 1, std::integral_constant<int, 1>());
         }
     } else {
         // blocks lo + 32 (wave + 4 i)
         const int32_t mine = lo + 32 * wave, n = mine < hi ? (hi - mine + 32 * kWaves - 1) / (32 * kWaves) : 0;
         stream_blocks<kBufs, 2 * kTile / TileLoad<D, 1>::kPer>(
             n, [&](int32_t i, int stage) { fetch(mine + 32 * kWaves * i, stage); },
-            [&](int32_t i, int stage) { compute(mine + 32 * kWaves * i, stage); });
+            [&](int32_t i, int stage) {
+                const uint32_t at = stage * 2 * kBytes;
+                w.template step<1>(in, at, at + kBytes, mine + 32 * kWaves * i, lim_first, c, lane);
+            });
     }
 
     const float2 ls = both_halves(w.l);
-    float l = ls.x + ls.y, m = w.m;
-    const float mc = m == -INFINITY ? -INFINITY : m * c;
+    float l = ls.x + ls.y, mc = w.m == -INFINITY ? -INFINITY : w.m * c;
     const int h = lane >> 5;
+    if constexpr (HALVES > 1) {
+        // the second half's sums to LDS, a piece of 32 columns at a time [wave][piece][4 registers][lane], then added
+        __shared__ float sm[kWaves][64], sl[kWaves][64];
+        static_assert(sizeof(sh) >= kWaves * kT * 4096, "room for the sums");
+        f32x4* const so = reinterpret_cast<f32x4*>(sh) + wave * kT * 256 + lane;
+        wait_and_sync();
+        if (half == 1) {
+            sm[wave][lane] = mc;
+            sl[wave][lane] = l;
+#pragma unroll
+            for (int t = 0; t < kT; ++t)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    so[t * 256 + r * 64] = f32x4{w.o[t][4 * r], w.o[t][4 * r + 1], w.o[t][4 * r + 2], w.o[t][4 * r + 3]};
+        }
+        wait_and_sync();
+        if (half == 1) return;
+        const float mo = sm[wave][lane], top = fmaxf(mc, mo);
+        const float f = mc == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mc - top), g = mo == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mo - top);
+        l = l * f + sl[wave][lane] * g;
+        mc = top;
+#pragma unroll
+        for (int t = 0; t < kT; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+                const f32x4 x = so[t * 256 + r * 16];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) w.o[t][r + e] = w.o[t][r + e] * f + x[e] * g;
+            }
+    }
     const int64_t job = (int64_t)a.first_job + blockIdx.x;
     if constexpr (ROWS == 128) {
         if (!live) return;
@@ -330,10 +365,12 @@ hipError_t launch_fwd(const FullCall& f, const FullPlan& p, float* part_o, float
         a.s = l.seqs;
         a.first_job = l.first_job;
         a.fold = l.fold;
-        if (p.rows == 128)
-            hipLaunchKernelGGL((full_fwd_kernel<T, D, 128>), dim3(l.jobs), dim3(256), 0, stream, a);
+        if (p.rows == 128 && p.halves == 2)
+            hipLaunchKernelGGL((full_fwd_kernel<T, D, 128, 2>), dim3(l.jobs), dim3(512), 0, stream, a);
+        else if (p.rows == 128)
+            hipLaunchKernelGGL((full_fwd_kernel<T, D, 128, 1>), dim3(l.jobs), dim3(256), 0, stream, a);
         else
-            hipLaunchKernelGGL((full_fwd_kernel<T, D, 32>), dim3(l.jobs), dim3(256), 0, stream, a);
+            hipLaunchKernelGGL((full_fwd_kernel<T, D, 32, 1>), dim3(l.jobs), dim3(256), 0, stream, a);
         hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
         if (l.tile_jobs > 0) {

@@ -62,6 +62,7 @@ struct FullLaunch {
 
 struct FullPlan {
     int32_t rows = 0;    // rows (or keys) of a tile, 128 or 32
+    int32_t halves = 1;  // groups of four waves that share a tile's streamed rows, 2 or 1
     int32_t split = 0;   // streamed rows of a run, 0: not split
     int64_t jobs = 0;
     std::vector<FullLaunch> launches;
