@@ -23,7 +23,7 @@ struct BwdArgs {
     const char *q, *k, *v, *dout;
     const uint16_t* out;
     const float* lse;
-    float *lse2, *D;                          // [Nq, H]: lse log2 e (+inf for a row that sees no key), D
+    float *lse2, *D;                          // [Nq, H]: lse log2 e (+inf for a row that sees no key), -D
     uint16_t *dq, *dk, *dv_out;
     float *part_dq, *part_dk, *part_dv;       // runs: [job][rows][width] sums
     int64_t q_row, q_head, k_row, k_head, v_row, v_head, do_row, do_head;   // bytes between tokens, heads
@@ -77,7 +77,7 @@ __global__ __launch_bounds__(256 * HALVES, ROWS == 128 ? 2 : 1) void full_dq_ker
     const float lse2 = lse == -INFINITY ? INFINITY : lse * kLog2e;
     if (live && lane < 32 && (ROWS == 128 ? half == 0 : wave == 0) && j.run == 0) {
         a.lse2[at] = lse2;
-        a.D[at] = di;
+        a.D[at] = -di;
     }
     const float c = a.scale * kLog2e;
     const int32_t lim = sees(row), lim_first = sees(row0), lim_last = row0 < nrows ? sees(row0 + 31) : 0;
@@ -102,18 +102,22 @@ __global__ __launch_bounds__(256 * HALVES, ROWS == 128 ? 2 : 1) void full_dq_ker
     for (int t = 0; t < kT; ++t) clear(acc[t]);
     Operands<D> in;
     in.init(base, lane);
+    // dp - D comes out of the product, which starts at -D (where there are registers for it)
+    constexpr bool kStart = D < 128;
+    f32x16 start;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) start[r] = kStart ? -di : 0.0f;
     auto compute = [&](int32_t key0, auto k_at, auto v_at) {
 #pragma unroll
         for (int b = 0; b < kTile / 32; ++b) {
             f32x16 s, dp;
             clear(s);
-            clear(dp);
 #pragma unroll
             for (int t = 0; t < D / 16; ++t) s = T::mfma(in.rows(t, k_at + b * 64 * D), q[t], s);
 #pragma unroll
-            for (int t = 0; t < D / 16; ++t) dp = T::mfma(in.rows(t, v_at + b * 64 * D), g[t], dp);
+            for (int t = 0; t < D / 16; ++t) dp = T::mfma(in.rows(t, v_at + b * 64 * D), g[t], t == 0 ? start : dp);
 #pragma unroll
-            for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], c, -lse2)) * (dp[r] - di);
+            for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], c, -lse2)) * (kStart ? dp[r] : dp[r] - di);
             if (key0 + 32 * b + 32 > lim_first) {
                 const int32_t left = lim - key0 - 32 * b - 4 * (lane >> 5);
 #pragma unroll
@@ -197,7 +201,7 @@ __global__ __launch_bounds__(256 * HALVES, KEYS == 128 ? 2 : 1) void full_dkv_ke
     constexpr int kT = D < 32 ? 1 : D / 32;
     __shared__ __attribute__((aligned(1024))) char sh[kOwn * kBufs * 2 * kBytes];   // [buffer][Q, dout]
     __shared__ __attribute__((aligned(1024))) s16x8 kept[kHeld ? 1 : kWaves * 2 * kSteps * 64];   // [wave][K's, V's][lane]
-    __shared__ __attribute__((aligned(16))) float st[kOwn][kBufs][2][kTile];   // [buffer][lse log2 e, D]
+    __shared__ __attribute__((aligned(16))) float st[kOwn][kBufs][2][kTile];   // [buffer][lse log2 e, -D]
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6 & 3);
     const int half = HALVES > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 8) : 0;
@@ -258,14 +262,24 @@ __global__ __launch_bounds__(256 * HALVES, KEYS == 128 ? 2 : 1) void full_dkv_ke
 #pragma unroll
         for (int b = 0; b < kTile / 32; ++b) {
             f32x16 s, dp;
+            const float* sb = &stats[buf][0][32 * b + 4 * (lane >> 5)];
             clear(s);
+            // dp - D comes out of the product, which starts at -D (where there are registers for it)
+            constexpr bool kStart = D < 128;
             clear(dp);
+            if constexpr (kStart) {
+#pragma unroll
+                for (int r = 0; r < 16; r += 4) {
+                    const f32x4 di = *reinterpret_cast<const f32x4*>(sb + kTile + 2 * r);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) dp[r + e] = di[e];
+                }
+            }
 #pragma unroll
             for (int t = 0; t < D / 16; ++t) s = T::mfma(in.rows(t, q_at + b * 64 * D), kHeld ? k[t] : own[t * 64], s);
 #pragma unroll
             for (int t = 0; t < D / 16; ++t)
                 dp = T::mfma(in.rows(t, g_at + b * 64 * D), kHeld ? v[t] : own[(kSteps + t) * 64], dp);
-            const float* sb = &stats[buf][0][32 * b + 4 * (lane >> 5)];
 #pragma unroll
             for (int r = 0; r < 16; r += 4) {
                 const f32x4 l = *reinterpret_cast<const f32x4*>(sb + 2 * r);
@@ -283,9 +297,10 @@ __global__ __launch_bounds__(256 * HALVES, KEYS == 128 ? 2 : 1) void full_dkv_ke
             }
 #pragma unroll
             for (int r = 0; r < 16; r += 4) {
-                const f32x4 di = *reinterpret_cast<const f32x4*>(sb + kTile + 2 * r);
+                f32x4 di = {0.0f, 0.0f, 0.0f, 0.0f};
+                if constexpr (!kStart) di = *reinterpret_cast<const f32x4*>(sb + kTile + 2 * r);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) dp[r + e] = s[r + e] * (dp[r + e] - di[e]);
+                for (int e = 0; e < 4; ++e) dp[r + e] = s[r + e] * (dp[r + e] + di[e]);
             }
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
@@ -385,13 +400,14 @@ __global__ __launch_bounds__(256 * HALVES, KEYS == 128 ? 2 : 1) void full_dkv_ke
 }
 
 struct SumArgs {
-    const float* part;          // [job][rows][width]
-    uint16_t* to;
+    const float* part[2];       // [job][rows][width], one or (dK, dV) two of them
+    uint16_t* to[2];
+    int32_t width[2];
+    float scale[2];
     FullSeqs s;                 // the sequences with several runs, a job for each tile and key head
     int32_t part0[kFullSeqs];
-    int32_t first_job, rows, width, split, Hk, rep;
+    int32_t first_job, rows, split, Hk, rep;
     bool causal, fold, keys;    // keys: rows are keys of the slot, else (token, head) pairs
-    float scale;
 };
 
 // Adds the runs of a tile in their order.
@@ -402,29 +418,28 @@ __global__ __launch_bounds__(256) void full_sum_kernel(const SumArgs a) {
     const int32_t runs = full_runs(a.keys ? (int64_t)a.s.q_len[s] * a.rep : a.s.k_len[s], a.split);
     const int32_t kv_head = (blockIdx.x - a.s.job0[s]) % a.Hk, place = (blockIdx.x - a.s.job0[s]) / a.Hk;
     const int32_t tile = full_tile(place, (nrows - 1) / a.rows + 1, a.causal, a.keys, a.fold);
-    const int groups = a.width / 4;
+    const int which = blockIdx.z, width = a.width[which], groups = width / 4;
     const int i = blockIdx.y * 256 + threadIdx.x, rr = i / groups, g = i % groups;
     const int32_t row = tile * a.rows + rr;
     if (rr >= a.rows || row >= nrows) return;
-    const float* p = a.part + (((int64_t)a.first_job + a.part0[s] + (int64_t)place * runs * a.Hk + kv_head) * a.rows + rr) * a.width + 4 * g;
-    const int64_t step = (int64_t)a.Hk * a.rows * a.width;
+    const float* p = a.part[which] + (((int64_t)a.first_job + a.part0[s] + (int64_t)place * runs * a.Hk + kv_head) * a.rows + rr) * width + 4 * g;
+    const int64_t step = (int64_t)a.Hk * a.rows * width;
     f32x4 x = *reinterpret_cast<const f32x4*>(p);
 #pragma unroll 4
     for (int32_t r = 1; r < runs; ++r) x += *reinterpret_cast<const f32x4*>(p + r * step);
     const int64_t at = a.keys ? (a.s.k_lo[s] + (int64_t)row) * a.Hk + kv_head
                               : (a.s.q_lo[s] + (int64_t)(row / a.rep)) * (a.Hk * a.rep) + kv_head * a.rep + row % a.rep;
-    *reinterpret_cast<s16x4*>(a.to + at * a.width + 4 * g) = round4<T>(x, a.scale);
+    *reinterpret_cast<s16x4*>(a.to[which] + at * width + 4 * g) = round4<T>(x, a.scale[which]);
 }
 
 template <typename T>
-hipError_t launch_sum(const BwdArgs& a, const FullLaunch& l, const FullPlan& p, const float* part, uint16_t* to, int32_t width,
-                      bool keys, float scale, hipStream_t stream) {
-    SumArgs b{};
-    b.part = part, b.to = to, b.s = l.tiles;
+hipError_t launch_sum(SumArgs& b, const BwdArgs& a, const FullLaunch& l, const FullPlan& p, bool keys, hipStream_t stream) {
+    b.s = l.tiles;
     for (int i = 0; i < kFullSeqs; ++i) b.part0[i] = l.part0[i];
-    b.first_job = l.first_job, b.rows = p.rows, b.width = width, b.split = p.split, b.Hk = a.Hk, b.rep = a.rep;
-    b.causal = a.causal, b.fold = l.fold, b.keys = keys, b.scale = scale;
-    hipLaunchKernelGGL((full_sum_kernel<T>), dim3(l.tile_jobs, (p.rows * (width / 4) + 255) / 256), dim3(256), 0, stream, b);
+    b.first_job = l.first_job, b.rows = p.rows, b.split = p.split, b.Hk = a.Hk, b.rep = a.rep;
+    b.causal = a.causal, b.fold = l.fold, b.keys = keys;
+    const int32_t widest = b.width[0] > b.width[1] ? b.width[0] : b.width[1];
+    hipLaunchKernelGGL((full_sum_kernel<T>), dim3(l.tile_jobs, (p.rows * (widest / 4) + 255) / 256, keys ? 2 : 1), dim3(256), 0, stream, b);
     return hipGetLastError();
 }
 
@@ -457,7 +472,10 @@ hipError_t launch_bwd(const FullCall& f, const FullPlan& dq, const FullPlan& dkv
         else
             hipLaunchKernelGGL((full_dq_kernel<T, D, 32, 1>), dim3(l.jobs), dim3(256), 0, stream, a);
         hipError_t e = hipGetLastError();
-        if (e == hipSuccess && l.tile_jobs > 0) e = launch_sum<T>(a, l, dq, ws.dq, a.dq, f.d, false, f.scale, stream);
+        if (e == hipSuccess && l.tile_jobs > 0) {
+            SumArgs b{{ws.dq}, {a.dq}, {f.d}, {f.scale}};
+            e = launch_sum<T>(b, a, l, dq, false, stream);
+        }
         if (e != hipSuccess) return e;
     }
     for (const FullLaunch& l : dkv.launches) {
@@ -469,8 +487,10 @@ hipError_t launch_bwd(const FullCall& f, const FullPlan& dq, const FullPlan& dkv
         else
             hipLaunchKernelGGL((full_dkv_kernel<T, D, 32, 1>), dim3(l.jobs), dim3(256), 0, stream, a);
         hipError_t e = hipGetLastError();
-        if (e == hipSuccess && l.tile_jobs > 0) e = launch_sum<T>(a, l, dkv, ws.dk, a.dk, f.d, true, f.scale, stream);
-        if (e == hipSuccess && l.tile_jobs > 0) e = launch_sum<T>(a, l, dkv, ws.dv, a.dv_out, f.dv, true, 1.0f, stream);
+        if (e == hipSuccess && l.tile_jobs > 0) {
+            SumArgs b{{ws.dk, ws.dv}, {a.dk, a.dv_out}, {f.d, f.dv}, {f.scale, 1.0f}};
+            e = launch_sum<T>(b, a, l, dkv, true, stream);
+        }
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
