@@ -87,8 +87,8 @@ bool finite_bits(float x) {   // (the sources are built without NaN tests)
 // Cuts the list of sequences, with tiles_of(seq) tiles (of all key heads) of
 // streamed_of(seq) streamed rows each, into launches, the costliest sequences
 // first (ties in their order), so that the last jobs are short ones.
-template <typename Tiles, typename Streamed>
-kmip_status_t cut(std::vector<Seq>& seqs, bool causal, const Tiles& tiles_of, const Streamed& streamed_of, FullPlan* p) {
+template <typename Tiles, typename Kept, typename Streamed>
+kmip_status_t cut(std::vector<Seq>& seqs, bool causal, const Tiles& tiles_of, const Kept& kept_of, const Streamed& streamed_of, FullPlan* p) {
     auto cost = [](const Seq& s) { return (int64_t)std::max(s.q_len, 1) * std::max(s.k_len, 1); };
     std::stable_sort(seqs.begin(), seqs.end(), [&](const Seq& x, const Seq& y) { return cost(x) > cost(y); });
     p->jobs = 0;
@@ -113,6 +113,7 @@ kmip_status_t cut(std::vector<Seq>& seqs, bool causal, const Tiles& tiles_of, co
                 l.part0[put(l.tiles, s, tile_jobs)] = (int32_t)jobs;
                 tile_jobs += tiles;
                 l.runs = std::max(l.runs, runs);
+                l.tile_rows = (int32_t)std::max<int64_t>(l.tile_rows, std::min<int64_t>(p->rows, kept_of(s)));
             }
             jobs += tiles * runs;
             if (p->jobs + jobs >= (int64_t(1) << 31) - 1) return record_error(KMIP_ERR_INVALID_ARG, "too many rows and key runs for one call");
@@ -165,7 +166,7 @@ kmip_status_t plan(std::vector<Seq>& seqs, int32_t Hk, bool causal, const Kept& 
         run = std::max<int64_t>(round_up(work / kSlots, 128), 512);
     static_assert(2 * 512 >= KMIP_FULL_LONG, "streams below are not cut");
     p->split = run > 0 && longest >= 2 * run ? (int32_t)std::min<int64_t>(run, INT32_MAX) : 0;
-    return cut(seqs, causal, [&](const Seq& s) { return tiles(s, p->rows); }, streamed_of, p);
+    return cut(seqs, causal, [&](const Seq& s) { return tiles(s, p->rows); }, kept_of, streamed_of, p);
 }
 
 kmip_status_t plan_rows(const Sequences& sq, int32_t H, int32_t Hk, bool causal, int32_t width, FullPlan* p) {

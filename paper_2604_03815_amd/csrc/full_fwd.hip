@@ -295,54 +295,72 @@ struct JoinArgs {
     int32_t lanes;              // threads that share a row's four columns, a power of two
 };
 
-// Joins the runs of row tiles.  A thread takes four columns of a row
-// and every lanes-th run; its sum, then the threads' in order.
+// Joins the runs of row tiles.  A thread takes four columns of a row and every
+// lanes-th run in one pass (reference, sum of weights, sums), then the threads
+// of a row are joined in their order.
 template <typename T>
 __global__ __launch_bounds__(256) void full_join_kernel(const JoinArgs b) {
-    const int32_t ROWS = b.rows;
     const FwdArgs& a = b.f;
     __shared__ f32x4 part[256];
     __shared__ float sm[256], sl[256];
     const int s = __builtin_amdgcn_readfirstlane(seq_of_job(a.s, blockIdx.x, threadIdx.x & 63));
     const int32_t q_lo = a.s.q_lo[s], nrows = a.s.q_len[s] * a.rep, runs = full_runs(a.s.k_len[s], a.split);
-    const int32_t tiles = (nrows + ROWS - 1) / ROWS, kv_head = (blockIdx.x - a.s.job0[s]) % a.Hk, place = (blockIdx.x - a.s.job0[s]) / a.Hk;
+    const int32_t tiles = (nrows - 1) / b.rows + 1, kv_head = (blockIdx.x - a.s.job0[s]) % a.Hk, place = (blockIdx.x - a.s.job0[s]) / a.Hk;
     const int32_t tile = full_tile(place, tiles, a.causal, false, a.fold);
-    const int groups = a.dv / 4;
-    const int g = threadIdx.x % groups, t = threadIdx.x / groups % b.lanes, rr = threadIdx.x / groups / b.lanes + blockIdx.y * (256 / groups / b.lanes);
-    const int32_t row = tile * ROWS + rr;
-    const bool live = rr < ROWS && row < nrows;
+    const int groups = a.dv / 4, at_once = 256 / groups / b.lanes;
+    const int g = threadIdx.x % groups, t = threadIdx.x / groups % b.lanes;
     // run 0; run r is r * Hk jobs on
-    const int64_t job = (int64_t)a.first_job + b.part0[s] + (int64_t)place * runs * a.Hk + kv_head;
-    const float2* ml = reinterpret_cast<const float2*>(a.part_ml) + job * ROWS + rr;
-    const float* po = a.part_o + (job * ROWS + rr) * a.dv + 4 * g;
-    const int64_t step = (int64_t)a.Hk * ROWS;
-    float top = -INFINITY;
-    if (live)
-        for (int32_t r = t; r < runs; r += b.lanes) top = fmaxf(top, ml[r * step].x);
-    sm[threadIdx.x] = top;
-    __syncthreads();
-    const int first = threadIdx.x - t * groups;
-    for (int u = 0; u < b.lanes; ++u) top = fmaxf(top, sm[first + u * groups]);
-    f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
-    float sum = 0.0f;
-    if (live && top != -INFINITY)
-        for (int32_t r = t; r < runs; r += b.lanes) {
-            const float2 m = ml[r * step];
-            const float f = __builtin_amdgcn_exp2f(m.x - top);
-            sum = fmaf(m.y, f, sum);
-            x += f * *reinterpret_cast<const f32x4*>(po + r * step * a.dv);
+    const int64_t job = (int64_t)a.first_job + b.part0[s] + (int64_t)place * runs * a.Hk + kv_head, step = (int64_t)a.Hk * b.rows;
+    const int32_t left = min(b.rows, nrows - tile * b.rows);
+    for (int32_t r0 = blockIdx.y * at_once; r0 < left; r0 += gridDim.y * at_once) {
+        const int32_t rr = r0 + threadIdx.x / groups / b.lanes, row = tile * b.rows + rr;
+        const bool live = rr < left;
+        const float2* ml = reinterpret_cast<const float2*>(a.part_ml) + job * b.rows + rr;
+        const float* po = a.part_o + (job * b.rows + rr) * a.dv + 4 * g;
+        float top = -INFINITY, sum = 0.0f;
+        f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+        auto add = [&](float m, float l, const f32x4& y) {   // m: -inf for a run without a key that the row sees
+            const float to = fmaxf(fmaxf(top, m), -1e30f), f = __builtin_amdgcn_exp2f(top - to), h = __builtin_amdgcn_exp2f(m - to);
+            top = fmaxf(top, m);
+            sum = sum * f + l * h;
+            x = x * f + y * h;
+        };
+        auto stream = [&](auto ahead) {   // that many runs' loads go out together
+            constexpr int kAhead = decltype(ahead)::value;
+            for (int32_t r0 = t; r0 < runs; r0 += kAhead * b.lanes) {
+                float2 m[kAhead];
+                f32x4 y[kAhead];
+#pragma unroll
+                for (int u = 0; u < kAhead; ++u) {
+                    const int64_t r = min(r0 + u * b.lanes, runs - 1);
+                    m[u] = ml[r * step];
+                    y[u] = *reinterpret_cast<const f32x4*>(po + r * step * a.dv);
+                }
+#pragma unroll
+                for (int u = 0; u < kAhead; ++u) add(r0 + u * b.lanes < runs ? m[u].x : -INFINITY, m[u].y, y[u]);
+            }
+        };
+        if (live) {
+            if (runs > 2 * b.lanes)
+                stream(std::integral_constant<int, 8>());
+            else
+                stream(std::integral_constant<int, 1>());
         }
-    part[threadIdx.x] = x;
-    sl[threadIdx.x] = sum;
-    __syncthreads();
-    if (!live || t != 0) return;
-    for (int u = 1; u < b.lanes; ++u) {
-        x += part[threadIdx.x + u * groups];
-        sum += sl[threadIdx.x + u * groups];
+        part[threadIdx.x] = x;
+        sm[threadIdx.x] = top;
+        sl[threadIdx.x] = sum;
+        __syncthreads();
+        if (live && t == 0) {
+            for (int u = 1; u < b.lanes; ++u) {
+                const int i = threadIdx.x + u * groups;
+                add(sm[i], sl[i], part[i]);
+            }
+            const int64_t at = (q_lo + (int64_t)(row / a.rep)) * a.H + kv_head * a.rep + row % a.rep;
+            *reinterpret_cast<s16x4*>(a.out + at * a.dv + 4 * g) = round4<T>(x, sum > 0.0f ? 1.0f / sum : 0.0f);
+            if (g == 0) a.lse[at] = sum > 0.0f ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
+        }
+        __syncthreads();
     }
-    const int64_t at = (q_lo + (int64_t)(row / a.rep)) * a.H + kv_head * a.rep + row % a.rep;
-    *reinterpret_cast<s16x4*>(a.out + at * a.dv + 4 * g) = round4<T>(x, sum > 0.0f ? 1.0f / sum : 0.0f);
-    if (g == 0) a.lse[at] = sum > 0.0f ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
 }
 
 template <typename T, int D>
@@ -382,8 +400,10 @@ hipError_t launch_fwd(const FullCall& f, const FullPlan& p, float* part_o, float
             b.rows = p.rows;
             b.lanes = 1;
             while (2 * b.lanes <= l.runs && 2 * b.lanes * groups <= 256) b.lanes *= 2;
-            const int at_once = 256 / groups / b.lanes;   // rows a workgroup takes
-            hipLaunchKernelGGL((full_join_kernel<T>), dim3(l.tile_jobs, (p.rows + at_once - 1) / at_once), dim3(256), 0, stream, b);
+            // a workgroup takes this many rows at a time; more than eight workgroups a CU do several rounds
+            const int at_once = 256 / groups / b.lanes, rounds = (l.tile_rows + at_once - 1) / at_once;
+            const int ny = rounds < 2048 / l.tile_jobs + 1 ? rounds : 2048 / l.tile_jobs + 1;
+            hipLaunchKernelGGL((full_join_kernel<T>), dim3(l.tile_jobs, ny), dim3(256), 0, stream, b);
             if ((e = hipGetLastError()) != hipSuccess) return e;
         }
     }

@@ -54,10 +54,10 @@ struct FullLaunch {
     int32_t jobs, first_job;
     bool fold;              // tiles in the order of full_tile()'s fold
     // the launch that joins runs: the sequences that have several, with a job for
-    // each tile and key head; most runs among them
+    // each tile and key head; most rows of a tile and most runs among them
     FullSeqs tiles;
     int32_t part0[kFullSeqs];   // their first jobs in the launch above
-    int32_t tile_jobs, runs;
+    int32_t tile_jobs, tile_rows, runs;
 };
 
 struct FullPlan {
