@@ -169,7 +169,8 @@ def compare_dense(args):
     inputs.  Dense attention is torch's scaled_dot_product_attention held to
     its flash / memory-efficient kernels (linear memory, no N x N matrix);
     the math fallback is not allowed, so a size it cannot take is reported
-    as an error rather than timed on another algorithm."""
+    as an error rather than timed on another algorithm.  The library's own
+    full attention (full_fwd, full_bwd) is timed on the same sizes."""
     import numpy as np
     import torch
     from torch.nn.attention import SDPBackend, sdpa_kernel
@@ -209,6 +210,12 @@ def compare_dense(args):
         row["kmip_training_peak_bytes"] = _peak_bytes(kmip_train) + ws.buf.numel() + 4 * (
             out.numel() + idx.numel() + lse.numel() + sum(x.numel() for x in grads))
         if e <= args.dense_max + 1e-9:
+            def full_train():
+                o, l = kmip.full_fwd(q, k, v, scale)
+                kmip.full_bwd(q, k, v, g, o, l, scale)
+
+            row["full_inference_ms"] = _time_ms(lambda: kmip.full_fwd(q, k, v, scale), reps)
+            row["full_training_ms"] = _time_ms(full_train, reps)
             # [batch 1, heads 1, N, d]
             qd, kd, vd, gd = (x.view(N, d).unsqueeze(0).unsqueeze(0) for x in (q, k, v, g))
             try:

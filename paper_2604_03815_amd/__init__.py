@@ -25,7 +25,7 @@ __all__ = [
     "KmipError", "MAX_K", "MAX_K_WIDE", "NOALLOC_SCRATCH_BYTES", "topk", "topk_prefilter", "topk_prefilter_workspace_size", "attend", "fwd", "fwd_noalloc", "bwd",
     "attention", "topk_workspace_size", "bwd_workspace_size", "Workspace", "load", "KMIPAttention",
     "linear_k_schedule", "full_fwd", "full_fwd_workspace_size", "full_bwd", "full_bwd_workspace_size",
-    "full_attention", "rotary", "rotary_frequencies",
+    "full_attention", "rotary", "rotary_frequencies", "Rotary", "FullAttention",
 ]
 
 
@@ -354,5 +354,5 @@ def _attention_function():
 
 
 from .full import full_attention, full_bwd, full_bwd_workspace_size, full_fwd, full_fwd_workspace_size  # noqa: E402
-from .rotary import rotary, rotary_frequencies  # noqa: E402
-from .layer import KMIPAttention, linear_k_schedule  # noqa: E402
+from .rotary import Rotary, rotary, rotary_frequencies  # noqa: E402
+from .layer import FullAttention, KMIPAttention, linear_k_schedule  # noqa: E402

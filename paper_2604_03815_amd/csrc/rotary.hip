@@ -80,8 +80,9 @@ __device__ __forceinline__ void sin_cos(uint32_t phase, float* s, float* c) {
     const uint32_t quarter = (phase + 0x20000000u) >> 30;
     const float x = (float)(int32_t)(phase - (quarter << 30)) * 1.4629180792671596e-9f;   // 2 pi / 2^32
     const float z = x * x;
-    const float sn = x + x * z * (-1.0f / 6 + z * (1.0f / 120 + z * (-1.0f / 5040 + z * (1.0f / 362880))));
-    const float cs = 1.0f + z * (-0.5f + z * (1.0f / 24 + z * (-1.0f / 720 + z * (1.0f / 40320 - z * (1.0f / 3628800)))));
+    // (fused steps written out, here and in turn(): every form rounds alike)
+    const float sn = fmaf(x * z, fmaf(z, fmaf(z, fmaf(z, 1.0f / 362880, -1.0f / 5040), 1.0f / 120), -1.0f / 6), x);
+    const float cs = fmaf(z, fmaf(z, fmaf(z, fmaf(z, fmaf(z, -1.0f / 3628800, 1.0f / 40320), -1.0f / 720), 1.0f / 24), -0.5f), 1.0f);
     const float u = (quarter & 1) ? cs : sn, w = (quarter & 1) ? sn : cs;
     *s = (quarter & 2) ? -u : u;
     *c = ((quarter + 1) & 2) ? -w : w;
@@ -91,9 +92,9 @@ __device__ __forceinline__ void sin_cos(uint32_t phase, float* s, float* c) {
 template <int P, bool INTER>
 __device__ __forceinline__ void turn(float (&u)[P], float (&v)[P], const float (&c)[P], const float (&s)[P]) {
     auto pair = [](float& a, float& b, float cs, float sn) {
-        const float f = a * cs - b * sn;
-        b = b * cs + a * sn;
-        a = f;
+        const float bs = b * sn, as = a * sn;
+        a = fmaf(a, cs, -bs);
+        b = fmaf(b, cs, as);
     };
 #pragma unroll
     for (int e = 0; e < P; ++e) {

@@ -135,7 +135,8 @@ def _inputs(q, k_, v):
 def _scratch(workspace, nbytes, device):
     if nbytes == 0:
         return None
-    if workspace is None:
+    # (a captured call keeps its addresses: it gets memory of its own, which no later call grows or shares)
+    if workspace is None or torch.cuda.is_current_stream_capturing():
         return torch.empty(nbytes, dtype=torch.uint8, device=device)
     buf = workspace.get(nbytes)
     if buf.device != device:
@@ -170,7 +171,7 @@ def full_fwd(q, k_, v, scale: float, graph_offsets: Optional[Sequence[int]] = No
         out = torch.empty((Nq, H, dv), dtype=q.dtype, device=dev)
     if lse is None:
         lse = torch.empty((Nq, H), dtype=torch.float32, device=dev)
-    _launch(dev, lib.kmip_full_fwd, q.data_ptr(), k_.data_ptr(), v.data_ptr(), code, _strides(q, k_, v), *ptrs, G, *sizes, scale,
+    _launch(dev, lib.kmip_full_fwd, q.data_ptr(), k_.data_ptr(), v.data_ptr(), code, _strides(q, k_, v), *ptrs, G, *sizes, float(scale),
             1 if causal else 0, out.data_ptr(), lse.data_ptr(), _address(buf), 0 if buf is None else buf.numel())
     return out, lse
 
@@ -205,7 +206,7 @@ def full_bwd(q, k_, v, dout, out, lse, scale: float, graph_offsets: Optional[Seq
     if dv is None:
         dv = torch.empty((Nk, Hk, wv), dtype=q.dtype, device=dev)
     _launch(dev, lib.kmip_full_bwd, q.data_ptr(), k_.data_ptr(), v.data_ptr(), dout.data_ptr(), out.data_ptr(), lse.data_ptr(),
-            code, _strides(q, k_, v, dout), *ptrs, G, *sizes, scale, 1 if causal else 0, dq.data_ptr(), dk.data_ptr(),
+            code, _strides(q, k_, v, dout), *ptrs, G, *sizes, float(scale), 1 if causal else 0, dq.data_ptr(), dk.data_ptr(),
             dv.data_ptr(), _address(buf), 0 if buf is None else buf.numel())
     return dq, dk, dv
 
@@ -217,7 +218,10 @@ def full_attention(q, k_, v, scale: float, graph_offsets: Optional[Sequence[int]
     The forward is ``full_fwd``; autograd's backward calls ``full_bwd`` with
     the saved out and lse.  Once differentiable.
     """
-    where = dict(graph_offsets=graph_offsets, key_offsets=key_offsets, key_lengths=key_lengths, causal=causal)
+    # (copies: the caller may change its own before the backward)
+    where = {n: None if x is None else np.array(x) for n, x in (("graph_offsets", graph_offsets), ("key_offsets", key_offsets),
+                                                                ("key_lengths", key_lengths))}
+    where["causal"] = causal
     return _full_function().apply(q, k_, v, scale, where, workspace)
 
 

@@ -48,6 +48,20 @@ def rotary_frequencies(rot: int, base: float = 10000.0, scaling: str = "none", f
     return freqs * keep + freqs / factor * (1.0 - keep), 0.1 * math.log(factor) + 1.0
 
 
+class Rotary:
+    """Frequencies and layout of rotary positions, for the layers: a call turns q and k (see ``rotary``).
+
+    rot: dimensions turned; the other arguments as in ``rotary_frequencies``.
+    """
+
+    def __init__(self, rot: int, interleaved: bool = False, **scaling):
+        self.freqs, self.magnitude = rotary_frequencies(rot, **scaling)
+        self.rot, self.interleaved = rot, interleaved
+
+    def __call__(self, q, k_=None, positions=None, dtype=None):
+        return rotary(q, k_, positions, self.freqs, interleaved=self.interleaved, magnitude=self.magnitude, dtype=dtype)
+
+
 def _rows(t, name):
     if not isinstance(t, torch.Tensor) or t.dim() != 3:
         raise ValueError(f"{name} must be a tensor [N, heads, d]")
