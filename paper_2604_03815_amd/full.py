@@ -32,28 +32,34 @@ _HALF = {torch.bfloat16: BF16, torch.float16: FP16}
 
 
 def _check_tensor(t, name, dtype, shape):
-    """A tensor of this type and shape whose last dimension is contiguous."""
+    """A tensor of this type and shape whose last dimension is contiguous; whether all of it is."""
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch tensor")
     if t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
     if t.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
-    if not t.is_contiguous() and t.shape[-1] > 1 and t.stride(-1) != 1 and t.numel():
+    if t.is_contiguous():
+        return True
+    if t.shape[-1] > 1 and t.stride(-1) != 1 and t.numel():
         raise ValueError(f"{name}: the last dimension must be contiguous")
+    return False
 
 
 def _check_output(t, name, dtype, shape):
-    if t is not None:
-        _check_tensor(t, name, dtype, shape)
-        if not t.is_contiguous():
-            raise ValueError(f"{name} must be contiguous")
+    if t is not None and not _check_tensor(t, name, dtype, shape):
+        raise ValueError(f"{name} must be contiguous")
+
+
+def _new(like, shape, dtype):
+    """A contiguous tensor of this shape and type on like's device (the cheapest way to it)."""
+    if like.shape == shape and like.dtype == dtype:
+        return torch.empty_like(like, memory_format=torch.contiguous_format)
+    return like.new_empty(shape, dtype=dtype)
 
 
 def _strides(*tensors):
-    """Host int64 pairs of strides, or None where all are contiguous."""
-    if all(t.is_contiguous() for t in tensors):
-        return None
+    """Host int64 pairs of strides."""
     s = [x for t in tensors for x in t.stride()[:2]]
     return (ctypes.c_int64 * len(s))(*s)
 
@@ -97,7 +103,7 @@ class _Ints:
                 if a.size and (int(a.min()) < -(1 << 31) or int(a.max()) >= 1 << 31):
                     raise OverflowError
                 a = np.ascontiguousarray(a, dtype=np.int32)
-                self.ptr, self.count = a.ctypes.data, len(a)
+                self.ptr, self.count = a.__array_interface__["data"][0], len(a)
         except (TypeError, OverflowError):
             raise ValueError(f"{name} must be a 1-D sequence of 32-bit integers") from None
         if self.count < 2 if n is None else self.count != n:
@@ -117,19 +123,20 @@ def _sequences(graph_offsets, key_offsets, key_lengths):
 
 
 def _inputs(q, k_, v):
-    """Checks Q, K and V; returns (Nq, Nk, H, Hk, d, dv) and the dtype's code."""
+    """Checks Q, K and V; returns (Nq, Nk, H, Hk, d, dv), the dtype's code and whether all are contiguous."""
     for t, name in ((q, "Q"), (k_, "K"), (v, "V")):
         if not isinstance(t, torch.Tensor) or t.dim() != 3:
             raise ValueError(f"{name} must be a tensor [N, heads, width]")
-    code = _HALF.get(q.dtype)
+    dtype = q.dtype
+    code = _HALF.get(dtype)
     if code is None:
-        raise TypeError(f"Q must be torch.bfloat16 or torch.float16, got {q.dtype}")
+        raise TypeError(f"Q must be torch.bfloat16 or torch.float16, got {dtype}")
     Nq, H, d = q.shape
     Nk, Hk, dv = v.shape
-    _check_tensor(q, "Q", q.dtype, (Nq, H, d))
-    _check_tensor(k_, "K", q.dtype, (Nk, Hk, d))
-    _check_tensor(v, "V", q.dtype, (Nk, Hk, dv))
-    return (Nq, Nk, H, Hk, d, dv), code
+    whole = _check_tensor(q, "Q", dtype, (Nq, H, d))
+    whole &= _check_tensor(k_, "K", dtype, (Nk, Hk, d))
+    whole &= _check_tensor(v, "V", dtype, (Nk, Hk, dv))
+    return (Nq, Nk, H, Hk, d, dv), code, whole
 
 
 def _scratch(workspace, nbytes, device):
@@ -157,7 +164,7 @@ def full_fwd_workspace_size(Nq: int, Nk: int, H: int, Hk: int, d: int, dv: int, 
 def full_fwd(q, k_, v, scale: float, graph_offsets: Optional[Sequence[int]] = None, key_offsets=None, key_lengths=None,
              causal: bool = False, out=None, lse=None, workspace=None):
     """Full softmax attention: returns (out, lse)."""
-    sizes, code = _inputs(q, k_, v)
+    sizes, code, whole = _inputs(q, k_, v)
     Nq, Nk, H, Hk, d, dv = sizes
     _check_output(out, "out", q.dtype, (Nq, H, dv))
     _check_output(lse, "lse", torch.float32, (Nq, H))
@@ -168,10 +175,10 @@ def full_fwd(q, k_, v, scale: float, graph_offsets: Optional[Sequence[int]] = No
     if Nk >= FULL_LONG:
         buf = _scratch(workspace, lib.kmip_full_fwd_workspace_size(*ptrs, G, *sizes), dev)
     if out is None:
-        out = torch.empty((Nq, H, dv), dtype=q.dtype, device=dev)
+        out = _new(q, (Nq, H, dv), q.dtype)
     if lse is None:
-        lse = torch.empty((Nq, H), dtype=torch.float32, device=dev)
-    _launch(dev, lib.kmip_full_fwd, q.data_ptr(), k_.data_ptr(), v.data_ptr(), code, _strides(q, k_, v), *ptrs, G, *sizes, float(scale),
+        lse = q.new_empty((Nq, H), dtype=torch.float32)
+    _launch(dev, lib.kmip_full_fwd, q.data_ptr(), k_.data_ptr(), v.data_ptr(), code, None if whole else _strides(q, k_, v), *ptrs, G, *sizes, float(scale),
             1 if causal else 0, out.data_ptr(), lse.data_ptr(), _address(buf), 0 if buf is None else buf.numel())
     return out, lse
 
@@ -185,12 +192,12 @@ def full_bwd_workspace_size(Nq: int, Nk: int, H: int, Hk: int, d: int, dv: int, 
 def full_bwd(q, k_, v, dout, out, lse, scale: float, graph_offsets: Optional[Sequence[int]] = None, key_offsets=None,
              key_lengths=None, causal: bool = False, dq=None, dk=None, dv=None, workspace=None):
     """Gradients of full softmax attention: returns (dQ, dK, dV) of the inputs' type."""
-    sizes, code = _inputs(q, k_, v)
+    sizes, code, whole = _inputs(q, k_, v)
     Nq, Nk, H, Hk, d, wv = sizes
-    _check_tensor(dout, "dOut", q.dtype, (Nq, H, wv))
+    whole &= _check_tensor(dout, "dOut", q.dtype, (Nq, H, wv))
     for t, name, dtype, shape in ((out, "out", q.dtype, (Nq, H, wv)), (lse, "lse", torch.float32, (Nq, H))):
-        _check_tensor(t, name, dtype, shape)
-        _check_output(t, name, dtype, shape)
+        if not _check_tensor(t, name, dtype, shape):
+            raise ValueError(f"{name} must be contiguous")
     _check_output(dq, "dQ", q.dtype, (Nq, H, d))
     _check_output(dk, "dK", q.dtype, (Nk, Hk, d))
     _check_output(dv, "dV", q.dtype, (Nk, Hk, wv))
@@ -200,13 +207,13 @@ def full_bwd(q, k_, v, dout, out, lse, scale: float, graph_offsets: Optional[Seq
     lib = load()
     buf = _scratch(workspace, lib.kmip_full_bwd_workspace_size(*ptrs, G, *sizes), dev)
     if dq is None:
-        dq = torch.empty((Nq, H, d), dtype=q.dtype, device=dev)
+        dq = _new(q, (Nq, H, d), q.dtype)
     if dk is None:
-        dk = torch.empty((Nk, Hk, d), dtype=q.dtype, device=dev)
+        dk = _new(k_, (Nk, Hk, d), q.dtype)
     if dv is None:
-        dv = torch.empty((Nk, Hk, wv), dtype=q.dtype, device=dev)
+        dv = _new(v, (Nk, Hk, wv), q.dtype)
     _launch(dev, lib.kmip_full_bwd, q.data_ptr(), k_.data_ptr(), v.data_ptr(), dout.data_ptr(), out.data_ptr(), lse.data_ptr(),
-            code, _strides(q, k_, v, dout), *ptrs, G, *sizes, float(scale), 1 if causal else 0, dq.data_ptr(), dk.data_ptr(),
+            code, None if whole else _strides(q, k_, v, dout), *ptrs, G, *sizes, float(scale), 1 if causal else 0, dq.data_ptr(), dk.data_ptr(),
             dv.data_ptr(), _address(buf), 0 if buf is None else buf.numel())
     return dq, dk, dv
 

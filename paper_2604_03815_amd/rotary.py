@@ -7,7 +7,6 @@ passed on.  The scores of turned queries and keys depend on the difference of th
 """
 from __future__ import annotations
 
-import ctypes
 import functools
 import math
 from typing import Optional
@@ -16,7 +15,7 @@ import numpy as np
 import torch
 
 from ._lib import load
-from .full import _DTYPES, _address, _check_devices, _check_tensor, _launch as _launch_on
+from .full import _DTYPES, _address, _check_devices, _check_tensor, _launch as _launch_on, _new, _strides
 
 
 def rotary_frequencies(rot: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0,
@@ -99,48 +98,46 @@ def _launch(q, k_, positions, freqs, interleaved, magnitude, inverse, dtype, q_o
     if f.ndim != 1:
         raise ValueError("freqs must be 1-D")
     N, H, d = q.shape
-    H2 = 0
+    H2, whole = 0, True
     if k_ is not None:
         _rows(k_, "k")
         H2 = k_.shape[1]
-        _check_tensor(k_, "k", q.dtype, (N, H2, d))
+        whole = _check_tensor(k_, "k", q.dtype, (N, H2, d))
     elif k_out is not None:
         raise ValueError("k_out without k")
-    _check_tensor(q, "q", q.dtype, (N, H, d))
     to = q.dtype if dtype is None else dtype
     if to not in _DTYPES:
         raise TypeError(f"dtype must be bfloat16, float16 or float32, got {to}")
-    _check_out(q_out, "q_out", to, (N, H, d))
-    _check_out(k_out, "k_out", to, (N, H2, d))
+    whole &= _check_tensor(q, "q", q.dtype, (N, H, d))
+    whole &= _check_out(q_out, "q_out", to, (N, H, d))
+    whole &= _check_out(k_out, "k_out", to, (N, H2, d))
     if positions is not None:
         _check_positions(positions, N)
     dev = _check_devices((q, "q"), (k_, "k"), (q_out, "q_out"), (k_out, "k_out"), (positions, "positions"))
     if q_out is None:
-        q_out = torch.empty((N, H, d), dtype=to, device=dev)
+        q_out = _new(q, (N, H, d), to)
     if k_ is not None and k_out is None:
-        k_out = torch.empty((N, H2, d), dtype=to, device=dev)
-    tensors = (q, q_out) if k_ is None else (q, q_out, k_, k_out)
+        k_out = _new(k_, (N, H2, d), to)
     strides = None
-    if not all(t.is_contiguous() for t in tensors):
-        s = [x for t in tensors for x in t.stride()[:2]]
-        strides = (ctypes.c_int64 * 8)(*s)
+    if not whole:
+        strides = _strides(q, q_out) if k_ is None else _strides(q, q_out, k_, k_out)
     _launch_on(dev, load().kmip_rotary, q.data_ptr(), q_out.data_ptr(), H, _address(k_), _address(k_out), H2, _DTYPES[q.dtype],
-               _DTYPES[to], strides, _address(positions), f.ctypes.data, N, d, 2 * len(f), 1 if interleaved else 0, magnitude,
-               1 if inverse else 0)
+               _DTYPES[to], strides, _address(positions), f.__array_interface__["data"][0], N, d, 2 * len(f), 1 if interleaved else 0,
+               float(magnitude), 1 if inverse else 0)
     return q_out if k_ is None else (q_out, k_out)
 
 
 def _check_out(t, name, dtype, shape):
-    if t is None:
-        return
-    _check_tensor(t, name, dtype, shape)
+    if t is None or _check_tensor(t, name, dtype, shape):
+        return True
     N, heads, d = shape
-    if t.numel() and not t.is_contiguous():
+    if t.numel():
         rows, cols = (t.stride(0), N), (t.stride(1), heads)
         # one of the two dimensions within the other's steps, rows of d values within the smaller's
         inner, outer = sorted(x for x in (rows, cols) if x[1] > 1) if N > 1 and heads > 1 else ((d, 1), max(rows, cols, key=lambda x: x[1]))
         if inner[0] < d or (outer[1] > 1 and outer[0] < (inner[1] - 1) * inner[0] + d):
             raise ValueError(f"{name} overlaps itself")
+    return False
 
 
 def _check_positions(positions, N):
