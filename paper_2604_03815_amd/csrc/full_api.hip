@@ -141,7 +141,7 @@ int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 //     and the last ones take half as long (8 heads, causal, forward: 8192 tokens,
 //     d = 128 182 us with one group, 165 with two; 16 heads, 4096 tokens, d = 64 65 and 56;
 //     but 4096 tokens of 8 heads at d = 128 91 and 98, 17 prompts of 2000, d = 64 229 and 246, since the groups'
-//     sums have to be added).  only_halves: the kernel has only that form.
+//     sums have to be added).  width: d + d_V; only_halves: the kernel has only that form.
 //   32 rows otherwise, in runs of at least 512 where that makes more jobs.
 // Runs cost the sums' way through memory, so that there are as few as fill the chip.
 template <typename Kept, typename Streamed>
@@ -158,7 +158,7 @@ kmip_status_t plan(std::vector<Seq>& seqs, int32_t Hk, bool causal, const Kept& 
     }
     const bool full = 2 * kept >= 128 * jobs;
     p->rows = full && (jobs >= kSlots || work >= kSlots * 512) ? 128 : 32;
-    p->halves = p->rows == 128 && (only_halves || (jobs <= 2 * kSlots && work >= jobs * (width == 128 ? 6144 : 1024))) ? 2 : 1;
+    p->halves = p->rows == 128 && (only_halves || (jobs <= 2 * kSlots && work >= jobs * (width > 192 ? 6144 : 1024))) ? 2 : 1;
     int64_t run = 0;
     if (p->rows == 32)
         run = std::max<int64_t>(round_up(work32 / (2 * kSlots), 128), 512);
@@ -183,7 +183,7 @@ kmip_status_t plan_keys(const Sequences& sq, int32_t H, int32_t Hk, bool causal,
     std::vector<Seq> seqs;
     for (int32_t g = 0; g < sq.count; ++g)
         if (sq.at(g).k_slot > 0) seqs.push_back(sq.at(g));
-    return plan(seqs, Hk, causal, [](const Seq& s) { return (int64_t)s.k_slot; }, [=](const Seq& s) { return s.q_len * rep; }, width, width == 128, p);
+    return plan(seqs, Hk, causal, [](const Seq& s) { return (int64_t)s.k_slot; }, [=](const Seq& s) { return s.q_len * rep; }, width, width == 256, p);
 }
 
 // Workspace of the forward: the runs' sums, then their maxima and sums of weights.
@@ -272,7 +272,7 @@ size_t kmip_full_fwd_workspace_size(const int32_t* q_offsets, const int32_t* k_o
         Sequences sq;
         FullPlan p;
         kmip_status_t e = check_call(q_offsets, k_offsets, k_lengths, num_seqs, Nq, Nk, H, Hk, d, dv, &sq);
-        if (e == KMIP_OK) e = plan_rows(sq, H, Hk, false, std::max(d, dv), &p);
+        if (e == KMIP_OK) e = plan_rows(sq, H, Hk, false, d + dv, &p);
         if (e == KMIP_OK) bytes = fwd_layout(p, dv).total;
         return e;
     });
@@ -294,7 +294,7 @@ kmip_status_t kmip_full_fwd(const void* Q, const void* K, const void* V, int32_t
         if (e == KMIP_OK) e = fill_call(Q, K, V, dtype, strides, Nq, Nk, H, Hk, d, dv, scale, causal, &f);
         if (e == KMIP_OK && Nq > 0 && (reinterpret_cast<uintptr_t>(out) & 15u) != 0)
             e = record_error(KMIP_ERR_INVALID_ARG, "out must be 16-byte aligned");
-        if (e == KMIP_OK) e = plan_rows(sq, H, Hk, causal != 0, std::max(d, dv), &p);
+        if (e == KMIP_OK) e = plan_rows(sq, H, Hk, causal != 0, d + dv, &p);
         if (e != KMIP_OK) return e;
         const FwdLayout L = fwd_layout(p, dv);
         if ((e = check_workspace(workspace, workspace_bytes, L.total)) != KMIP_OK) return e;
@@ -315,8 +315,8 @@ size_t kmip_full_bwd_workspace_size(const int32_t* q_offsets, const int32_t* k_o
         Sequences sq;
         FullPlan dq, dkv;
         kmip_status_t e = check_call(q_offsets, k_offsets, k_lengths, num_seqs, Nq, Nk, H, Hk, d, dv, &sq);
-        if (e == KMIP_OK) e = plan_rows(sq, H, Hk, false, std::max(d, dv), &dq);
-        if (e == KMIP_OK) e = plan_keys(sq, H, Hk, false, std::max(d, dv), &dkv);
+        if (e == KMIP_OK) e = plan_rows(sq, H, Hk, false, d + dv, &dq);
+        if (e == KMIP_OK) e = plan_keys(sq, H, Hk, false, d + dv, &dkv);
         if (e == KMIP_OK) bytes = bwd_layout(dq, dkv, Nq, H, d, dv).total;
         return e;
     });
@@ -342,8 +342,8 @@ kmip_status_t kmip_full_bwd(const void* Q, const void* K, const void* V, const v
         for (const void* p : {out, static_cast<const void*>(dQ), static_cast<const void*>(dK), static_cast<const void*>(dV)})
             if (e == KMIP_OK && (reinterpret_cast<uintptr_t>(p) & 15u) != 0)
                 e = record_error(KMIP_ERR_INVALID_ARG, "out, dQ, dK and dV must be 16-byte aligned");
-        if (e == KMIP_OK) e = plan_rows(sq, H, Hk, causal != 0, std::max(d, dv), &dq);
-        if (e == KMIP_OK) e = plan_keys(sq, H, Hk, causal != 0, std::max(d, dv), &dkv);
+        if (e == KMIP_OK) e = plan_rows(sq, H, Hk, causal != 0, d + dv, &dq);
+        if (e == KMIP_OK) e = plan_keys(sq, H, Hk, causal != 0, d + dv, &dkv);
         if (e != KMIP_OK) return e;
         const BwdLayout L = bwd_layout(dq, dkv, Nq, H, d, dv);
         if ((e = check_workspace(workspace, workspace_bytes, L.total)) != KMIP_OK) return e;

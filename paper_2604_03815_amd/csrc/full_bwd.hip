@@ -27,21 +27,19 @@ struct BwdArgs {
     uint16_t *dq, *dk, *dv_out;
     float *part_dq, *part_dk, *part_dv;       // runs: [job][rows][width] sums
     int64_t q_row, q_head, k_row, k_head, v_row, v_head, do_row, do_head;   // bytes between tokens, heads
-    int32_t H, Hk, rep, d, dv, split;
+    int32_t H, Hk, rep, split;
     bool causal, fold;
     float scale;
     int32_t first_job;
     FullSeqs s;
 };
 
-template <typename T, int D, int ROWS, int HALVES>
+template <typename T, int DK, int DV, int ROWS, int HALVES>
 __global__ __launch_bounds__(256 * HALVES, ROWS == 128 ? 2 : 1) void full_dq_kernel(const BwdArgs a) {
-    constexpr int kTile = ROWS == 128 ? (D == 16 ? 128 : 64) : 32;
-    constexpr int kBytes = kTile * 2 * D;
-    constexpr int kWaves = 4, kOwn = ROWS == 128 ? HALVES : kWaves;
-    constexpr int kBufs = ROWS == 128 ? 2 : kStages<D>;
-    constexpr int kT = D < 32 ? 1 : D / 32;
-    __shared__ __attribute__((aligned(1024))) char sh[kOwn * kBufs * 2 * kBytes];
+    using B = Buffers<DK, DV, ROWS == 128 ? (DK + DV == 32 ? 128 : 64) : 32>;   // [buffer][K, V]
+    constexpr int kTile = B::kTile, kWaves = 4, kOwn = ROWS == 128 ? HALVES : kWaves;
+    constexpr int kBufs = ROWS == 128 ? 2 : B::kOwnStages, kT = kPieces<DK>;
+    __shared__ __attribute__((aligned(1024))) char sh[kOwn * kBufs * B::kBytes];
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6 & 3);
     const int half = HALVES > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 8) : 0;
@@ -58,15 +56,15 @@ __global__ __launch_bounds__(256 * HALVES, ROWS == 128 ? 2 : 1) void full_dq_ker
     const int32_t token = min(row, nrows - 1) / a.rep, head = j.kv_head * a.rep + min(row, nrows - 1) % a.rep;
     const int64_t at = (j.q_lo + (int64_t)token) * a.H + head;
 
-    s16x8 q[D / 16], g[D / 16];
-    load_columns<D>(q, a.q + (j.q_lo + (int64_t)token) * a.q_row + head * a.q_head, a.d, lane);
-    load_columns<D>(g, a.dout + (j.q_lo + (int64_t)token) * a.do_row + head * a.do_head, a.dv, lane);
+    s16x8 q[DK / 16], g[DV / 16];
+    load_columns<DK>(q, a.q + (j.q_lo + (int64_t)token) * a.q_row + head * a.q_head, lane);
+    load_columns<DV>(g, a.dout + (j.q_lo + (int64_t)token) * a.do_row + head * a.do_head, lane);
     float di = 0.0f;
     {
-        s16x8 o[D / 16];
-        load_columns<D>(o, reinterpret_cast<const char*>(a.out + at * a.dv), a.dv, lane);
+        s16x8 o[DV / 16];
+        load_columns<DV>(o, reinterpret_cast<const char*>(a.out + at * DV), lane);
 #pragma unroll
-        for (int t = 0; t < D / 16; ++t)
+        for (int t = 0; t < DV / 16; ++t)
 #pragma unroll
             for (int e = 0; e < 8; ++e) di = fmaf(T::widen(g[t][e]), T::widen(o[t][e]), di);
         const float2 ds = both_halves(di);
@@ -87,35 +85,31 @@ __global__ __launch_bounds__(256 * HALVES, ROWS == 128 ? 2 : 1) void full_dq_ker
 
     const char* kp = a.k + (int64_t)j.k_lo * a.k_row + j.kv_head * a.k_head;
     const char* vp = a.v + (int64_t)j.k_lo * a.v_row + j.kv_head * a.v_head;
-    const uint32_t base = lds_addr(sh) + (ROWS == 128 ? half : wave) * kBufs * 2 * kBytes;
-    constexpr int kParts = ROWS == 128 ? kWaves : 1;
-    const int part = ROWS == 128 ? wave : 0;
-    TileLoad<D, kParts> kl, vl;
-    kl.init(lane, part, a.d, (uint32_t)a.k_row);
-    vl.init(lane, part, a.dv, (uint32_t)a.v_row);
+    const uint32_t base = lds_addr(sh) + (ROWS == 128 ? half : wave) * kBufs * B::kBytes;
+    PairLoad<B, DK, DV, ROWS == 128> load;
+    load.init(lane, wave, a.k_row, a.v_row);
     auto fetch = [&](int32_t key, int buf) {
-        kl.template issue<kTile>(base + buf * 2 * kBytes, kp + (int64_t)key * a.k_row, part, j.k_len - key);
-        vl.template issue<kTile>(base + buf * 2 * kBytes + kBytes, vp + (int64_t)key * a.v_row, part, j.k_len - key);
+        load.issue(base + buf * B::kBytes, kp + (int64_t)key * a.k_row, vp + (int64_t)key * a.v_row, j.k_len - key);
     };
     f32x16 acc[kT];
 #pragma unroll
     for (int t = 0; t < kT; ++t) clear(acc[t]);
-    Operands<D> in;
+    PairOperands<B, DK, DV> in;
     in.init(base, lane);
     // dp - D comes out of the product, which starts at -D (where there are registers for it)
-    constexpr bool kStart = D < 128;
+    constexpr bool kStart = DK + DV < 192;
     f32x16 start;
 #pragma unroll
     for (int r = 0; r < 16; ++r) start[r] = kStart ? -di : 0.0f;
-    auto compute = [&](int32_t key0, auto k_at, auto v_at) {
+    auto compute = [&](int32_t key0, auto at) {
 #pragma unroll
         for (int b = 0; b < kTile / 32; ++b) {
             f32x16 s, dp;
             clear(s);
 #pragma unroll
-            for (int t = 0; t < D / 16; ++t) s = T::mfma(in.rows(t, k_at + b * 64 * D), q[t], s);
+            for (int t = 0; t < DK / 16; ++t) s = T::mfma(in.x_rows(t, at + b * 64 * DK), q[t], s);
 #pragma unroll
-            for (int t = 0; t < D / 16; ++t) dp = T::mfma(in.rows(t, v_at + b * 64 * D), g[t], t == 0 ? start : dp);
+            for (int t = 0; t < DV / 16; ++t) dp = T::mfma(in.y_rows(t, at + b * 64 * DV), g[t], t == 0 ? start : dp);
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], c, -lse2)) * (kStart ? dp[r] : dp[r] - di);
             if (key0 + 32 * b + 32 > lim_first) {
@@ -128,7 +122,7 @@ __global__ __launch_bounds__(256 * HALVES, ROWS == 128 ? 2 : 1) void full_dq_ker
             for (int i = 0; i < 2; ++i) {
                 const s16x8 p = round8<T>(s, i);   // rounded to the inputs' type, the operand of the product
 #pragma unroll
-                for (int t = 0; t < kT; ++t) acc[t] = T::mfma(in.columns(t, k_at + (32 * b + 16 * i) * 2 * D), p, acc[t]);
+                for (int t = 0; t < kT; ++t) acc[t] = T::mfma(in.x_columns(t, at + (32 * b + 16 * i) * 2 * DK), p, acc[t]);
             }
         }
     };
@@ -141,7 +135,7 @@ __global__ __launch_bounds__(256 * HALVES, ROWS == 128 ? 2 : 1) void full_dq_ker
             wait_and_sync();
             if (i + 1 < mine) fetch(key + kTile, buf ^ 1);
             if (i < mine && key < lim_last)
-                compute(key, Constant<decltype(buf)::value * 2 * kBytes>(), Constant<decltype(buf)::value * 2 * kBytes + kBytes>());
+                compute(key, Constant<decltype(buf)::value * B::kBytes>());
         };
         for (int32_t i = 0; i < most; i += 2) {
             stage(i, std::integral_constant<int, 0>());
@@ -154,53 +148,48 @@ __global__ __launch_bounds__(256 * HALVES, ROWS == 128 ? 2 : 1) void full_dq_ker
 #pragma unroll
         for (int t = 0; t < kT; ++t) {
             if (j.runs > 1)
-                store_sums(a.part_dq + (job * ROWS + (row - j.tile * ROWS)) * a.d, acc[t], t, a.d, lane);
+                store_sums<DK>(a.part_dq + (job * ROWS + (row - j.tile * ROWS)) * DK, acc[t], t, lane);
             else
-                store_piece<T>(a.dq + at * a.d, acc[t], t, a.scale, a.d, lane);
+                store_piece<T, DK>(a.dq + at * DK, acc[t], t, a.scale, lane);
         }
     } else {
         // blocks lo + 32 (wave + 4 i)
         const int32_t mine = lo + 32 * wave, n = mine < hi ? (hi - mine + 32 * kWaves - 1) / (32 * kWaves) : 0;
-        stream_blocks<kBufs, 2 * kTile / TileLoad<D, 1>::kPer>(
+        stream_blocks<kBufs, B::kOwnLoads>(
             n, [&](int32_t i, int stage) { fetch(mine + 32 * kWaves * i, stage); },
-            [&](int32_t i, int stage) {
-                const uint32_t at = stage * 2 * kBytes;
-                compute(mine + 32 * kWaves * i, at, at + kBytes);
-            });
+            [&](int32_t i, int stage) { compute(mine + 32 * kWaves * i, (uint32_t)stage * B::kBytes); });
         // the four waves' sums, in their order
         wait_and_sync();
         float* const so = reinterpret_cast<float*>(sh);
 #pragma unroll
-        for (int t = 0; t < kT; ++t) put_piece<D>(so + wave * 32 * D, acc[t], t, 1.0f, lane);
+        for (int t = 0; t < kT; ++t) put_piece<DK>(so + wave * 32 * DK, acc[t], t, 1.0f, lane);
         wait_and_sync();
-        for (int i = threadIdx.x; i < 32 * (D / 4); i += 256) {
-            const int rr = i / (D / 4), gg = i % (D / 4);
+        for (int i = threadIdx.x; i < 32 * (DK / 4); i += 256) {
+            const int rr = i / (DK / 4), gg = i % (DK / 4);
             const int32_t rowi = j.tile * ROWS + rr;
-            if (rowi >= nrows || 4 * gg >= a.d) continue;
-            f32x4 x = get_piece<D>(so, rr, gg);
+            if (rowi >= nrows) continue;
+            f32x4 x = get_piece<DK>(so, rr, gg);
 #pragma unroll
-            for (int u = 1; u < kWaves; ++u) x += get_piece<D>(so + u * 32 * D, rr, gg);
+            for (int u = 1; u < kWaves; ++u) x += get_piece<DK>(so + u * 32 * DK, rr, gg);
             const int64_t to = (j.q_lo + (int64_t)(rowi / a.rep)) * a.H + j.kv_head * a.rep + rowi % a.rep;
             if (j.runs > 1)
-                *reinterpret_cast<f32x4*>(a.part_dq + (((int64_t)a.first_job + blockIdx.x) * ROWS + rr) * a.d + 4 * gg) = x;
+                *reinterpret_cast<f32x4*>(a.part_dq + (((int64_t)a.first_job + blockIdx.x) * ROWS + rr) * DK + 4 * gg) = x;
             else
-                *reinterpret_cast<s16x4*>(a.dq + to * a.d + 4 * gg) = round4<T>(x, a.scale);
+                *reinterpret_cast<s16x4*>(a.dq + to * DK + 4 * gg) = round4<T>(x, a.scale);
         }
     }
 }
 
-template <typename T, int D, int KEYS, int HALVES>
+template <typename T, int DK, int DV, int KEYS, int HALVES>
 __global__ __launch_bounds__(256 * HALVES, KEYS == 128 ? 2 : 1) void full_dkv_kernel(const BwdArgs a) {
-    constexpr int kTile = KEYS == 128 ? (D == 16 ? 128 : D == 128 ? 32 : 64) : 32;   // tokens a buffer holds
-    // The kept K and V stay in registers, or are read from LDS where registers would spill
-    constexpr int kSteps = D / 16;
-    constexpr bool kHeld = KEYS == 32 || D < 128;
-    constexpr int kBytes = kTile * 2 * D;
-    constexpr int kWaves = 4, kOwn = KEYS == 128 ? HALVES : kWaves;
-    constexpr int kBufs = KEYS == 128 ? 2 : kStages<D>;
-    constexpr int kT = D < 32 ? 1 : D / 32;
-    __shared__ __attribute__((aligned(1024))) char sh[kOwn * kBufs * 2 * kBytes];   // [buffer][Q, dout]
-    __shared__ __attribute__((aligned(1024))) s16x8 kept[kHeld ? 1 : kWaves * 2 * kSteps * 64];   // [wave][K's, V's][lane]
+    // tokens a buffer holds: fewer where the kept K and V are in LDS too, which they
+    // are where registers would spill
+    constexpr bool kHeld = KEYS == 32 || DK + DV < 256;
+    using B = Buffers<DK, DV, KEYS == 128 ? (DK + DV == 32 ? 128 : kHeld ? 64 : 32) : 32>;   // [buffer][Q, dout]
+    constexpr int kTile = B::kTile, kWaves = 4, kOwn = KEYS == 128 ? HALVES : kWaves;
+    constexpr int kBufs = KEYS == 128 ? 2 : B::kOwnStages, kTK = kPieces<DK>, kTV = kPieces<DV>, kK = DK / 16, kV = DV / 16;
+    __shared__ __attribute__((aligned(1024))) char sh[kOwn * kBufs * B::kBytes];
+    __shared__ __attribute__((aligned(1024))) s16x8 kept[kHeld ? 1 : kWaves * (kK + kV) * 64];   // [wave][K's, V's][lane]
     __shared__ __attribute__((aligned(16))) float st[kOwn][kBufs][2][kTile];   // [buffer][lse log2 e, -D]
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6 & 3);
@@ -214,41 +203,43 @@ __global__ __launch_bounds__(256 * HALVES, KEYS == 128 ? 2 : 1) void full_dkv_ke
     const int32_t tile_lo = tile * KEYS;                       // keys from here on
     const int32_t key0 = tile_lo + (KEYS == 128 ? 32 * wave : 0), key = key0 + (lane & 31);
     const int64_t key_at = min(key, max(k_len, 1) - 1);
-    s16x8 k[D / 16], v[D / 16];
+    s16x8 k[kK], v[kV];
     if (k_len > 0) {
-        load_columns<D>(k, a.k + (k_lo + key_at) * a.k_row + kv_head * a.k_head, a.d, lane);
-        load_columns<D>(v, a.v + (k_lo + key_at) * a.v_row + kv_head * a.v_head, a.dv, lane);
+        load_columns<DK>(k, a.k + (k_lo + key_at) * a.k_row + kv_head * a.k_head, lane);
+        load_columns<DV>(v, a.v + (k_lo + key_at) * a.v_row + kv_head * a.v_head, lane);
     } else {
 #pragma unroll
-        for (int t = 0; t < D / 16; ++t) k[t] = v[t] = s16x8{};
+        for (int t = 0; t < kK; ++t) k[t] = s16x8{};
+#pragma unroll
+        for (int t = 0; t < kV; ++t) v[t] = s16x8{};
     }
-    s16x8* const own = kept + (kHeld ? 0 : wave * 2 * kSteps * 64 + lane);   // (both halves')
+    s16x8* const own = kept + (kHeld ? 0 : wave * (kK + kV) * 64 + lane);   // (both halves')
     if (!kHeld && half == 0) {
 #pragma unroll
-        for (int t = 0; t < kSteps; ++t) own[t * 64] = k[t], own[(kSteps + t) * 64] = v[t];
+        for (int t = 0; t < kK; ++t) own[t * 64] = k[t];
+#pragma unroll
+        for (int t = 0; t < kV; ++t) own[(kK + t) * 64] = v[t];
     }
     // the first token that sees the tile, and its first and last key of this wave
     const int32_t t_lo = tile_lo >= k_len ? q_len : a.causal ? max(0, tile_lo - off) : 0;
     const int32_t t_wave = a.causal ? key0 - off : 0, t_all = a.causal ? key0 + 31 - off : 0;
     const float c = a.scale * kLog2e;
 
-    f32x16 dk[kT], dv[kT];
+    f32x16 dk[kTK], dv[kTV];
 #pragma unroll
-    for (int t = 0; t < kT; ++t) clear(dk[t]), clear(dv[t]);
-    const uint32_t base = lds_addr(sh) + (KEYS == 128 ? half : wave) * kBufs * 2 * kBytes;
+    for (int t = 0; t < kTK; ++t) clear(dk[t]);
+#pragma unroll
+    for (int t = 0; t < kTV; ++t) clear(dv[t]);
+    const uint32_t base = lds_addr(sh) + (KEYS == 128 ? half : wave) * kBufs * B::kBytes;
     float(*const stats)[2][kTile] = st[KEYS == 128 ? half : wave];
-    constexpr int kParts = KEYS == 128 ? kWaves : 1;
     const int part = KEYS == 128 ? wave : 0;
-    TileLoad<D, kParts> ql, gl;
-    ql.init(lane, part, a.d, (uint32_t)a.q_row);
-    gl.init(lane, part, a.dv, (uint32_t)a.do_row);
+    PairLoad<B, DK, DV, KEYS == 128> load;
+    load.init(lane, wave, a.q_row, a.do_row);
     const uint32_t st_base = lds_addr(stats);
     auto fetch = [&](int32_t hr, int32_t tok, int buf) {
         const int32_t head = kv_head * a.rep + hr;
-        ql.template issue<kTile>(base + buf * 2 * kBytes, a.q + (q_lo + (int64_t)tok) * a.q_row + head * a.q_head, part,
-                                 q_len - tok);
-        gl.template issue<kTile>(base + buf * 2 * kBytes + kBytes, a.dout + (q_lo + (int64_t)tok) * a.do_row + head * a.do_head,
-                                 part, q_len - tok);
+        load.issue(base + buf * B::kBytes, a.q + (q_lo + (int64_t)tok) * a.q_row + head * a.q_head,
+                   a.dout + (q_lo + (int64_t)tok) * a.do_row + head * a.do_head, q_len - tok);
         // the tokens' statistics, 64 values a wave
         if (part < kTile / 32) {
             const int i = 64 * part + lane;
@@ -256,16 +247,16 @@ __global__ __launch_bounds__(256 * HALVES, KEYS == 128 ? 2 : 1) void full_dkv_ke
             load_word_to_lds(st_base + buf * kTile * 8 + 256 * part, (i < kTile ? a.lse2 : a.D) + at);
         }
     };
-    Operands<D> in;
+    PairOperands<B, DK, DV> in;
     in.init(base, lane);
-    auto compute = [&](int32_t tok, auto q_at, auto g_at, int buf) {
+    auto compute = [&](int32_t tok, auto at, int buf) {
 #pragma unroll
         for (int b = 0; b < kTile / 32; ++b) {
             f32x16 s, dp;
             const float* sb = &stats[buf][0][32 * b + 4 * (lane >> 5)];
             clear(s);
             // dp - D comes out of the product, which starts at -D (where there are registers for it)
-            constexpr bool kStart = D < 128;
+            constexpr bool kStart = DK + DV < 192;
             clear(dp);
             if constexpr (kStart) {
 #pragma unroll
@@ -276,10 +267,9 @@ __global__ __launch_bounds__(256 * HALVES, KEYS == 128 ? 2 : 1) void full_dkv_ke
                 }
             }
 #pragma unroll
-            for (int t = 0; t < D / 16; ++t) s = T::mfma(in.rows(t, q_at + b * 64 * D), kHeld ? k[t] : own[t * 64], s);
+            for (int t = 0; t < kK; ++t) s = T::mfma(in.x_rows(t, at + b * 64 * DK), kHeld ? k[t] : own[t * 64], s);
 #pragma unroll
-            for (int t = 0; t < D / 16; ++t)
-                dp = T::mfma(in.rows(t, g_at + b * 64 * D), kHeld ? v[t] : own[(kSteps + t) * 64], dp);
+            for (int t = 0; t < kV; ++t) dp = T::mfma(in.y_rows(t, at + b * 64 * DV), kHeld ? v[t] : own[(kK + t) * 64], dp);
 #pragma unroll
             for (int r = 0; r < 16; r += 4) {
                 const f32x4 l = *reinterpret_cast<const f32x4*>(sb + 2 * r);
@@ -306,9 +296,9 @@ __global__ __launch_bounds__(256 * HALVES, KEYS == 128 ? 2 : 1) void full_dkv_ke
             for (int i = 0; i < 2; ++i) {
                 const s16x8 p = round8<T>(s, i), x = round8<T>(dp, i);   // rounded, the operands of the products
 #pragma unroll
-                for (int t = 0; t < kT; ++t) {
-                    dv[t] = T::mfma(in.columns(t, g_at + (32 * b + 16 * i) * 2 * D), p, dv[t]);
-                    dk[t] = T::mfma(in.columns(t, q_at + (32 * b + 16 * i) * 2 * D), x, dk[t]);
+                for (int t = 0; t < (kTK > kTV ? kTK : kTV); ++t) {
+                    if (t < kTV) dv[t < kTV ? t : 0] = T::mfma(in.y_columns(t < kTV ? t : 0, at + (32 * b + 16 * i) * 2 * DV), p, dv[t < kTV ? t : 0]);
+                    if (t < kTK) dk[t < kTK ? t : 0] = T::mfma(in.x_columns(t < kTK ? t : 0, at + (32 * b + 16 * i) * 2 * DK), x, dk[t < kTK ? t : 0]);
                 }
             }
         }
@@ -336,66 +326,66 @@ __global__ __launch_bounds__(256 * HALVES, KEYS == 128 ? 2 : 1) void full_dkv_ke
                 fetch(hr, tok, buf ^ 1);
             }
             if (i < mine && now + kTile > t_wave)
-                compute(now, Constant<decltype(buf)::value * 2 * kBytes>(), Constant<decltype(buf)::value * 2 * kBytes + kBytes>(), decltype(buf)::value);
+                compute(now, Constant<decltype(buf)::value * B::kBytes>(), decltype(buf)::value);
         };
         for (int32_t i = 0; i < most; i += 2) {
             stage(i, std::integral_constant<int, 0>());
             if (i + 1 < most) stage(i + 1, std::integral_constant<int, 1>());
         }
         if constexpr (HALVES > 1) {
-            add_half<kT>(dk, sh, wave, half, lane);
-            if (!add_half<kT>(dv, sh, wave, half, lane)) return;
+            add_half<kTK>(dk, sh, wave, half, lane);
+            if (!add_half<kTV>(dv, sh, wave, half, lane)) return;
         }
         if (key >= slot) return;
         const int64_t at = (k_lo + (int64_t)key) * a.Hk + kv_head;
         // rows behind the keys in use have no gradient
         const bool used = key < k_len;
 #pragma unroll
-        for (int t = 0; t < kT; ++t) {
-            if (!used) clear(dk[t]), clear(dv[t]);
-            if (runs > 1) {
-                store_sums(a.part_dk + (job * KEYS + (key - tile_lo)) * a.d, dk[t], t, a.d, lane);
-                store_sums(a.part_dv + (job * KEYS + (key - tile_lo)) * a.dv, dv[t], t, a.dv, lane);
-                continue;
-            }
-            store_piece<T>(a.dk + at * a.d, dk[t], t, a.scale, a.d, lane);
-            store_piece<T>(a.dv_out + at * a.dv, dv[t], t, 1.0f, a.dv, lane);
+        for (int t = 0; t < kTK; ++t) {
+            if (!used) clear(dk[t]);
+            if (runs > 1)
+                store_sums<DK>(a.part_dk + (job * KEYS + (key - tile_lo)) * DK, dk[t], t, lane);
+            else
+                store_piece<T, DK>(a.dk + at * DK, dk[t], t, a.scale, lane);
+        }
+#pragma unroll
+        for (int t = 0; t < kTV; ++t) {
+            if (!used) clear(dv[t]);
+            if (runs > 1)
+                store_sums<DV>(a.part_dv + (job * KEYS + (key - tile_lo)) * DV, dv[t], t, lane);
+            else
+                store_piece<T, DV>(a.dv_out + at * DV, dv[t], t, 1.0f, lane);
         }
     } else {
         // tiles first + wave + 4 i
         const int32_t mine = n > wave ? (n - wave + kWaves - 1) / kWaves : 0;
         auto tok_of = [&](int32_t i) { return t_lo + (first + wave + kWaves * i) % per * kTile; };
-        stream_blocks<kBufs, 2 * kTile / TileLoad<D, 1>::kPer + 1>(
+        stream_blocks<kBufs, B::kOwnLoads + 1>(
             mine, [&](int32_t i, int stage) { fetch((first + wave + kWaves * i) / per, tok_of(i), stage); },
-            [&](int32_t i, int stage) {
-                const uint32_t at = stage * 2 * kBytes;
-                compute(tok_of(i), at, at + kBytes, stage);
-            });
+            [&](int32_t i, int stage) { compute(tok_of(i), (uint32_t)stage * B::kBytes, stage); });
         // the four waves' sums, in their order: dK, then dV
-        float* const so = reinterpret_cast<float*>(sh);
-#pragma unroll
-        for (int w = 0; w < 2; ++w) {
-            const int32_t width = w == 0 ? a.d : a.dv;
+        auto join = [&](auto& x, auto width, float* part, uint16_t* to, float f) {
+            constexpr int W = decltype(width)::value;
+            float* const so = reinterpret_cast<float*>(sh);
             wait_and_sync();
 #pragma unroll
-            for (int t = 0; t < kT; ++t) put_piece<D>(so + wave * 32 * D, w == 0 ? dk[t] : dv[t], t, 1.0f, lane);
+            for (int t = 0; t < kPieces<W>; ++t) put_piece<W>(so + wave * 32 * W, x[t], t, 1.0f, lane);
             wait_and_sync();
-            for (int i = threadIdx.x; i < 32 * (D / 4); i += 256) {
-                const int rr = i / (D / 4), gg = i % (D / 4);
-                if (tile_lo + rr >= slot || 4 * gg >= width) continue;
-                f32x4 y = get_piece<D>(so, rr, gg);
+            for (int i = threadIdx.x; i < 32 * (W / 4); i += 256) {
+                const int rr = i / (W / 4), gg = i % (W / 4);
+                if (tile_lo + rr >= slot) continue;
+                f32x4 y = get_piece<W>(so, rr, gg);
 #pragma unroll
-                for (int u = 1; u < kWaves; ++u) y += get_piece<D>(so + u * 32 * D, rr, gg);
+                for (int u = 1; u < kWaves; ++u) y += get_piece<W>(so + u * 32 * W, rr, gg);
                 if (tile_lo + rr >= k_len) y = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-                if (runs > 1) {
-                    *reinterpret_cast<f32x4*>((w == 0 ? a.part_dk : a.part_dv) + (job * KEYS + rr) * width + 4 * gg) = y;
-                    continue;
-                }
-                uint16_t* to = w == 0 ? a.dk : a.dv_out;
-                *reinterpret_cast<s16x4*>(to + ((k_lo + (int64_t)(tile_lo + rr)) * a.Hk + kv_head) * width + 4 * gg) =
-                    round4<T>(y, w == 0 ? a.scale : 1.0f);
+                if (runs > 1)
+                    *reinterpret_cast<f32x4*>(part + (job * KEYS + rr) * W + 4 * gg) = y;
+                else
+                    *reinterpret_cast<s16x4*>(to + ((k_lo + (int64_t)(tile_lo + rr)) * a.Hk + kv_head) * W + 4 * gg) = round4<T>(y, f);
             }
-        }
+        };
+        join(dk, std::integral_constant<int, DK>(), a.part_dk, a.dk, a.scale);
+        join(dv, std::integral_constant<int, DV>(), a.part_dv, a.dv_out, 1.0f);
     }
 }
 
@@ -443,7 +433,7 @@ hipError_t launch_sum(SumArgs& b, const BwdArgs& a, const FullLaunch& l, const F
     return hipGetLastError();
 }
 
-template <typename T, int D>
+template <typename T, int DK, int DV>
 hipError_t launch_bwd(const FullCall& f, const FullPlan& dq, const FullPlan& dkv, const FullBwdSpace& ws, hipStream_t stream) {
     BwdArgs a{};
     a.q = reinterpret_cast<const char*>(f.q);
@@ -461,16 +451,16 @@ hipError_t launch_bwd(const FullCall& f, const FullPlan& dq, const FullPlan& dkv
     a.k_row = 2 * f.k_row, a.k_head = 2 * f.k_head;
     a.v_row = 2 * f.v_row, a.v_head = 2 * f.v_head;
     a.do_row = 2 * f.do_row, a.do_head = 2 * f.do_head;
-    a.H = f.H, a.Hk = f.Hk, a.rep = f.H / f.Hk, a.d = f.d, a.dv = f.dv, a.causal = f.causal != 0;
+    a.H = f.H, a.Hk = f.Hk, a.rep = f.H / f.Hk, a.causal = f.causal != 0;
     a.scale = f.scale;
     for (const FullLaunch& l : dq.launches) {
         a.s = l.seqs, a.first_job = l.first_job, a.fold = l.fold, a.split = dq.split;
         if (dq.rows == 128 && dq.halves == 2)
-            hipLaunchKernelGGL((full_dq_kernel<T, D, 128, 2>), dim3(l.jobs), dim3(512), 0, stream, a);
+            hipLaunchKernelGGL((full_dq_kernel<T, DK, DV, 128, 2>), dim3(l.jobs), dim3(512), 0, stream, a);
         else if (dq.rows == 128)
-            hipLaunchKernelGGL((full_dq_kernel<T, D, 128, 1>), dim3(l.jobs), dim3(256), 0, stream, a);
+            hipLaunchKernelGGL((full_dq_kernel<T, DK, DV, 128, 1>), dim3(l.jobs), dim3(256), 0, stream, a);
         else
-            hipLaunchKernelGGL((full_dq_kernel<T, D, 32, 1>), dim3(l.jobs), dim3(256), 0, stream, a);
+            hipLaunchKernelGGL((full_dq_kernel<T, DK, DV, 32, 1>), dim3(l.jobs), dim3(256), 0, stream, a);
         hipError_t e = hipGetLastError();
         if (e == hipSuccess && l.tile_jobs > 0) {
             SumArgs b{{ws.dq}, {a.dq}, {f.d}, {f.scale}};
@@ -481,11 +471,11 @@ hipError_t launch_bwd(const FullCall& f, const FullPlan& dq, const FullPlan& dkv
     for (const FullLaunch& l : dkv.launches) {
         a.s = l.seqs, a.first_job = l.first_job, a.fold = l.fold, a.split = dkv.split;
         if (dkv.rows == 128 && dkv.halves == 2)
-            hipLaunchKernelGGL((full_dkv_kernel<T, D, 128, 2>), dim3(l.jobs), dim3(512), 0, stream, a);
+            hipLaunchKernelGGL((full_dkv_kernel<T, DK, DV, 128, 2>), dim3(l.jobs), dim3(512), 0, stream, a);
         else if (dkv.rows == 128)
-            hipLaunchKernelGGL((full_dkv_kernel<T, D, 128, D == 128 ? 2 : 1>), dim3(l.jobs), dim3(256), 0, stream, a);
+            hipLaunchKernelGGL((full_dkv_kernel<T, DK, DV, 128, DK + DV == 256 ? 2 : 1>), dim3(l.jobs), dim3(256), 0, stream, a);
         else
-            hipLaunchKernelGGL((full_dkv_kernel<T, D, 32, 1>), dim3(l.jobs), dim3(256), 0, stream, a);
+            hipLaunchKernelGGL((full_dkv_kernel<T, DK, DV, 32, 1>), dim3(l.jobs), dim3(256), 0, stream, a);
         hipError_t e = hipGetLastError();
         if (e == hipSuccess && l.tile_jobs > 0) {
             SumArgs b{{ws.dk, ws.dv}, {a.dk, a.dv_out}, {f.d, f.dv}, {f.scale, 1.0f}};
@@ -499,14 +489,15 @@ hipError_t launch_bwd(const FullCall& f, const FullPlan& dq, const FullPlan& dkv
 }  // namespace
 
 hipError_t launch_full_bwd(const FullCall& f, const FullPlan& dq, const FullPlan& dkv, const FullBwdSpace& ws, hipStream_t stream) {
-    const int32_t w = f.d > f.dv ? f.d : f.dv;
-#define KMIP_FULL_BWD(W) \
-    if (w == W) return f.fp16 ? launch_bwd<Fp16, W>(f, dq, dkv, ws, stream) : launch_bwd<Bf16, W>(f, dq, dkv, ws, stream);
+#define KMIP_FULL_CASE(DK, DV) \
+    if (f.d == DK && f.dv == DV) return f.fp16 ? launch_bwd<Fp16, DK, DV>(f, dq, dkv, ws, stream) : launch_bwd<Bf16, DK, DV>(f, dq, dkv, ws, stream);
+#define KMIP_FULL_BWD(DK) KMIP_FULL_CASE(DK, 16) KMIP_FULL_CASE(DK, 32) KMIP_FULL_CASE(DK, 64) KMIP_FULL_CASE(DK, 128)
     KMIP_FULL_BWD(16)
     KMIP_FULL_BWD(32)
     KMIP_FULL_BWD(64)
     KMIP_FULL_BWD(128)
 #undef KMIP_FULL_BWD
+#undef KMIP_FULL_CASE
     return hipErrorInvalidValue;
 }
 

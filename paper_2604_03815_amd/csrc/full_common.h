@@ -151,9 +151,6 @@ __device__ __forceinline__ void wait_and_sync() {
 
 // Loads tiles of rows of a strided tensor into LDS.  A round of PARTS
 // instructions (one from each of PARTS waves) writes PARTS * 512 / D rows.
-// Columns from `cols` on (there are some when the tensor is narrower than the
-// kernel's width) repeat the row's first chunk: they meet zeros in the other
-// operand, or make output columns that are not stored.
 template <int D, int PARTS>
 struct TileLoad {
     static constexpr int kPer = 512 / D * PARTS;            // rows of a round
@@ -162,13 +159,12 @@ struct TileLoad {
     uint32_t row;         // its row among them
     uint32_t stride;      // bytes between rows
 
-    __device__ __forceinline__ void init(int lane, int part, int32_t cols, uint32_t row_stride) {
+    __device__ __forceinline__ void init(int lane, int part, uint32_t row_stride) {
         row = part * (512 / D) + lane / (D / 8);
         stride = row_stride;
 #pragma unroll
         for (int v = 0; v < kVar; ++v) {
-            uint32_t c = (uint32_t)(lane & (D / 8 - 1)) ^ (uint32_t)swz<D>((int)row + v * kPer);
-            if ((int32_t)(8 * c) >= cols) c = 0;
+            const uint32_t c = (uint32_t)(lane & (D / 8 - 1)) ^ (uint32_t)swz<D>((int)row + v * kPer);
             off[v] = row * stride + 16 * c;
         }
     }
@@ -232,17 +228,11 @@ __device__ __forceinline__ RowJob row_job(const FullSeqs& seqs, int32_t Hk, int3
 }
 
 // The right operand of 32 columns from a strided tensor: this lane's row
-// (16-byte aligned, `cols` values), zeros behind its width.
+// (16-byte aligned).
 template <int D>
-__device__ __forceinline__ void load_columns(s16x8 (&x)[D / 16], const char* row, int32_t cols, int lane) {
+__device__ __forceinline__ void load_columns(s16x8 (&x)[D / 16], const char* row, int lane) {
 #pragma unroll
-    for (int t = 0; t < D / 16; ++t) {
-        const int col = 16 * t + 8 * (lane >> 5);
-        if (col < cols)
-            x[t] = *reinterpret_cast<const s16x8*>(row + 2 * col);
-        else
-            x[t] = s16x8{};
-    }
+    for (int t = 0; t < D / 16; ++t) x[t] = *reinterpret_cast<const s16x8*>(row + 2 * (16 * t + 8 * (lane >> 5)));
 }
 
 __device__ __forceinline__ void clear(f32x16& x) {
@@ -261,12 +251,12 @@ __device__ __forceinline__ s16x8 round8(const f32x16& x, int i) {
 
 // Stores column tile t of a transposed result (this lane's row at `row`),
 // times f.
-template <typename T>
-__device__ __forceinline__ void store_piece(uint16_t* row, const f32x16& x, int t, float f, int32_t cols, int lane) {
+template <typename T, int D>
+__device__ __forceinline__ void store_piece(uint16_t* row, const f32x16& x, int t, float f, int lane) {
 #pragma unroll
     for (int r = 0; r < 16; r += 4) {
         const int col = 32 * t + 2 * r + 4 * (lane >> 5);
-        if (col < cols) {
+        if (col < D) {
             s16x4 y;
 #pragma unroll
             for (int e = 0; e < 4; ++e) y[e] = T::round(x[r + e] * f);
@@ -276,11 +266,12 @@ __device__ __forceinline__ void store_piece(uint16_t* row, const f32x16& x, int 
 }
 
 // The same in float32, unrounded (a run's sums).
-__device__ __forceinline__ void store_sums(float* row, const f32x16& x, int t, int32_t cols, int lane) {
+template <int D>
+__device__ __forceinline__ void store_sums(float* row, const f32x16& x, int t, int lane) {
 #pragma unroll
     for (int r = 0; r < 16; r += 4) {
         const int col = 32 * t + 2 * r + 4 * (lane >> 5);
-        if (col < cols) *reinterpret_cast<f32x4*>(row + col) = f32x4{x[r], x[r + 1], x[r + 2], x[r + 3]};
+        if (col < D) *reinterpret_cast<f32x4*>(row + col) = f32x4{x[r], x[r + 1], x[r + 2], x[r + 3]};
     }
 }
 
@@ -292,11 +283,65 @@ __device__ __forceinline__ s16x4 round4(const f32x4& x, float f) {
     return y;
 }
 
-// Stages of LDS that a wave with buffers of its own keeps (two tensors of 32
-// rows each, 128 D bytes): deep enough for the loads' latency where a block
-// takes little time, few enough for several workgroups a CU.
+// Widths a kernel is built for: DK of queries and keys, DV of values.  How
+// the streamed rows lie in LDS: buffers of kTile rows of both tensors.
+template <int DK, int DV, int TILE>
+struct Buffers {
+    static constexpr int kTile = TILE, kFirst = TILE * 2 * DK, kBytes = kFirst + TILE * 2 * DV;   // the first tensor's, both tensors' bytes
+    // waves that load a tensor: all four, or two where its tile has only two loads
+    static constexpr int kPartsK = kFirst >= 4096 ? 4 : 2, kPartsV = TILE * 2 * DV >= 4096 ? 4 : 2;
+    // the same for a wave with buffers of its own: its loads
+    static constexpr int kOwnLoads = TILE / TileLoad<DK, 1>::kPer + TILE / TileLoad<DV, 1>::kPer;
+    // and its buffers: deep enough for the loads' latency where a block takes
+    // little time, few enough for several workgroups a CU
+    static constexpr int kOwnStages = DK + DV <= 32 ? 4 : DK + DV <= 64 ? 3 : 2;
+};
+
+// 32-wide pieces of a width.
 template <int D>
-constexpr int kStages = D == 16 ? 4 : D == 32 ? 3 : 2;
+constexpr int kPieces = D < 32 ? 1 : D / 32;
+
+// The left operands of both tensors of a buffer; tensors of one width share
+// their addresses, a constant distance apart.
+template <typename B, int DK, int DV>
+struct PairOperands {
+    Operands<DK> x;
+    Operands<DV> y;
+
+    __device__ __forceinline__ void init(uint32_t buffer, int lane) {
+        x.init(buffer, lane);
+        if constexpr (DK != DV) y.init(buffer + B::kFirst, lane);
+    }
+    __device__ __forceinline__ s16x8 x_rows(int t, uint32_t at) const { return x.rows(t, at); }
+    __device__ __forceinline__ s16x8 x_columns(int t, uint32_t at) const { return x.columns(t, at); }
+    __device__ __forceinline__ s16x8 y_rows(int t, uint32_t at) const {
+        if constexpr (DK == DV) return x.rows(t, at + B::kFirst);
+        return y.rows(t, at);
+    }
+    __device__ __forceinline__ s16x8 y_columns(int t, uint32_t at) const {
+        if constexpr (DK == DV) return x.columns(t, at + B::kFirst);
+        return y.columns(t, at);
+    }
+};
+
+// Loads a tile of both tensors: `shared`, each of four waves a part of it; else one wave all of it.
+template <typename B, int DK, int DV, bool SHARED>
+struct PairLoad {
+    TileLoad<DK, SHARED ? B::kPartsK : 1> x;
+    TileLoad<DV, SHARED ? B::kPartsV : 1> y;
+    int px, py;   // this wave's parts, negative: none
+
+    __device__ __forceinline__ void init(int lane, int wave, int64_t x_row, int64_t y_row) {
+        px = SHARED ? (wave < B::kPartsK ? wave : -1) : 0;
+        py = SHARED ? wave - (4 - B::kPartsV) : 0;
+        x.init(lane, px < 0 ? 0 : px, (uint32_t)x_row);
+        y.init(lane, py < 0 ? 0 : py, (uint32_t)y_row);
+    }
+    __device__ __forceinline__ void issue(uint32_t lds, const char* xp, const char* yp, int32_t left) const {
+        if (!SHARED || B::kPartsK == 4 || px >= 0) x.template issue<B::kTile>(lds, xp, px, left);
+        if (!SHARED || B::kPartsV == 4 || py >= 0) y.template issue<B::kTile>(lds + B::kFirst, yp, py, left);
+    }
+};
 
 // A wave's own stream: `fetch(i, stage)` issues block i's loads (LOADS
 // instructions), `use(i, stage)` computes on it, for i < n.

@@ -34,7 +34,7 @@ struct FwdArgs {
     float* lse;
     float *part_o, *part_ml;    // split: [job][ROWS][dv] sums, [job][ROWS][2] maximum (times c) and sum
     int64_t q_row, q_head, k_row, k_head, v_row, v_head;   // bytes between tokens, heads
-    int32_t H, Hk, rep, d, dv, split;
+    int32_t H, Hk, rep, dv, split;
     bool causal, fold;
     float scale;
     int32_t first_job;          // of the launch, among the call's
@@ -42,23 +42,23 @@ struct FwdArgs {
 };
 
 // A wave's running state: 32 columns of rows, two lanes a column.
-template <typename T, int D>
+template <typename T, int DK, int DV>
 struct FwdWave {
-    static constexpr int kT = D < 32 ? 1 : D / 32;   // 32-wide pieces of the value columns
-    s16x8 q[D / 16];
+    static constexpr int kT = kPieces<DV>;
+    s16x8 q[DK / 16];
     f32x16 o[kT];
     float m, l;     // reference of the weights, sum of this lane's
     int32_t lim;    // keys this row sees
 
-    // NB blocks of 32 keys from key0 on; keys and values at distances k_at and v_at.
-    template <int NB, typename KAt, typename VAt>
-    __device__ __forceinline__ void step(const Operands<D>& in, KAt k_at, VAt v_at, int32_t key0, int32_t lim_first, float c, int lane) {
+    // NB blocks of 32 keys from key0 on; keys and values at distance `at` from the operands' addresses.
+    template <int NB, typename In, typename At>
+    __device__ __forceinline__ void step(const In& in, At at, int32_t key0, int32_t lim_first, float c, int lane) {
         f32x16 s[NB];
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
             clear(s[b]);
 #pragma unroll
-            for (int t = 0; t < D / 16; ++t) s[b] = T::mfma(in.rows(t, k_at + b * 64 * D), q[t], s[b]);
+            for (int t = 0; t < DK / 16; ++t) s[b] = T::mfma(in.x_rows(t, at + b * 64 * DK), q[t], s[b]);
         }
         if (key0 + 32 * NB > lim_first) {
             const int32_t left = lim - key0 - 4 * (lane >> 5);
@@ -103,21 +103,19 @@ struct FwdWave {
                 // rounded to the inputs' type, the operand of the product: half a step of each weight
                 const s16x8 p = round8<T>(s[b], i);
 #pragma unroll
-                for (int t = 0; t < kT; ++t) o[t] = T::mfma(in.columns(t, v_at + (32 * b + 16 * i) * 2 * D), p, o[t]);
+                for (int t = 0; t < kT; ++t) o[t] = T::mfma(in.y_columns(t, at + (32 * b + 16 * i) * 2 * DV), p, o[t]);
             }
         }
     }
 };
 
-template <typename T, int D, int ROWS, int HALVES>
+template <typename T, int DK, int DV, int ROWS, int HALVES>
 __global__ __launch_bounds__(256 * HALVES, ROWS == 128 ? 2 : 1) void full_fwd_kernel(const FwdArgs a) {
-    constexpr int kTile = ROWS == 128 ? (D == 16 ? 128 : 64) : 32;   // keys a buffer holds
-    constexpr int kBytes = kTile * 2 * D;                            // of one tensor's buffer
-    constexpr int kWaves = 4, kOwn = ROWS == 128 ? HALVES : kWaves;  // buffer sets
-    constexpr int kBufs = ROWS == 128 ? 2 : kStages<D>;
-    constexpr int kT = FwdWave<T, D>::kT;
-    __shared__ __attribute__((aligned(1024))) char sh[kOwn * kBufs * 2 * kBytes];
-    static_assert(ROWS == 128 || sizeof(sh) >= 32 * D * 4 * kWaves, "room for the join");
+    using B = Buffers<DK, DV, ROWS == 128 ? (DK + DV == 32 ? 128 : 64) : 32>;   // [buffer][K, V]
+    constexpr int kTile = B::kTile, kWaves = 4, kOwn = ROWS == 128 ? HALVES : kWaves;   // buffer sets
+    constexpr int kBufs = ROWS == 128 ? 2 : B::kOwnStages, kT = kPieces<DV>;
+    __shared__ __attribute__((aligned(1024))) char sh[kOwn * kBufs * B::kBytes];
+    static_assert(ROWS == 128 || sizeof(sh) >= 32 * DV * 4 * kWaves, "room for the join");
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6 & 3);
     const int half = HALVES > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 8) : 0;
@@ -133,8 +131,8 @@ __global__ __launch_bounds__(256 * HALVES, ROWS == 128 ? 2 : 1) void full_fwd_ke
     const bool live = row < nrows;
     const int32_t token = min(row, nrows - 1) / a.rep, head = j.kv_head * a.rep + min(row, nrows - 1) % a.rep;
 
-    FwdWave<T, D> w;
-    load_columns<D>(w.q, a.q + (j.q_lo + (int64_t)token) * a.q_row + head * a.q_head, a.d, lane);
+    FwdWave<T, DK, DV> w;
+    load_columns<DK>(w.q, a.q + (j.q_lo + (int64_t)token) * a.q_row + head * a.q_head, lane);
 #pragma unroll
     for (int t = 0; t < kT; ++t) clear(w.o[t]);
     w.m = -INFINITY;
@@ -148,17 +146,13 @@ __global__ __launch_bounds__(256 * HALVES, ROWS == 128 ? 2 : 1) void full_fwd_ke
     const float c = a.scale * kLog2e;
     const char* kp = a.k + (int64_t)j.k_lo * a.k_row + j.kv_head * a.k_head;
     const char* vp = a.v + (int64_t)j.k_lo * a.v_row + j.kv_head * a.v_head;
-    const uint32_t base = lds_addr(sh) + (ROWS == 128 ? half : wave) * kBufs * 2 * kBytes;   // [buffer][K, V]
-    constexpr int kParts = ROWS == 128 ? kWaves : 1;
-    const int part = ROWS == 128 ? wave : 0;
-    TileLoad<D, kParts> kl, vl;
-    kl.init(lane, part, a.d, (uint32_t)a.k_row);
-    vl.init(lane, part, a.dv, (uint32_t)a.v_row);
+    const uint32_t base = lds_addr(sh) + (ROWS == 128 ? half : wave) * kBufs * B::kBytes;
+    PairLoad<B, DK, DV, ROWS == 128> load;
+    load.init(lane, wave, a.k_row, a.v_row);
     auto fetch = [&](int32_t key, int buf) {
-        kl.template issue<kTile>(base + buf * 2 * kBytes, kp + (int64_t)key * a.k_row, part, j.k_len - key);
-        vl.template issue<kTile>(base + buf * 2 * kBytes + kBytes, vp + (int64_t)key * a.v_row, part, j.k_len - key);
+        load.issue(base + buf * B::kBytes, kp + (int64_t)key * a.k_row, vp + (int64_t)key * a.v_row, j.k_len - key);
     };
-    Operands<D> in;
+    PairOperands<B, DK, DV> in;
     in.init(base, lane);
     if constexpr (ROWS == 128) {
         // each half takes its part of the tiles; the first one's is as long or one longer
@@ -170,7 +164,7 @@ __global__ __launch_bounds__(256 * HALVES, ROWS == 128 ? 2 : 1) void full_fwd_ke
             wait_and_sync();
             if (i + 1 < mine) fetch(key + kTile, buf ^ 1);
             if (i < mine && key < lim_last)
-                w.template step<kTile / 32>(in, Constant<decltype(buf)::value * 2 * kBytes>(), Constant<decltype(buf)::value * 2 * kBytes + kBytes>(), key, lim_first, c, lane);
+                w.template step<kTile / 32>(in, Constant<decltype(buf)::value * B::kBytes>(), key, lim_first, c, lane);
         };
         for (int32_t i = 0; i < most; i += 2) {
             stage(i, std::integral_constant<int, 0>());
@@ -179,11 +173,10 @@ __global__ __launch_bounds__(256 * HALVES, ROWS == 128 ? 2 : 1) void full_fwd_ke
     } else {
         // blocks lo + 32 (wave + 4 i)
         const int32_t mine = lo + 32 * wave, n = mine < hi ? (hi - mine + 32 * kWaves - 1) / (32 * kWaves) : 0;
-        stream_blocks<kBufs, 2 * kTile / TileLoad<D, 1>::kPer>(
+        stream_blocks<kBufs, B::kOwnLoads>(
             n, [&](int32_t i, int stage) { fetch(mine + 32 * kWaves * i, stage); },
             [&](int32_t i, int stage) {
-                const uint32_t at = stage * 2 * kBytes;
-                w.template step<1>(in, at, at + kBytes, mine + 32 * kWaves * i, lim_first, c, lane);
+                w.template step<1>(in, (uint32_t)stage * B::kBytes, mine + 32 * kWaves * i, lim_first, c, lane);
             });
     }
 
@@ -224,9 +217,9 @@ __global__ __launch_bounds__(256 * HALVES, ROWS == 128 ? 2 : 1) void full_fwd_ke
     if constexpr (ROWS == 128) {
         if (!live) return;
         if (j.runs > 1) {
-            float* po = a.part_o + (job * ROWS + (row - j.tile * ROWS)) * a.dv;
+            float* po = a.part_o + (job * ROWS + (row - j.tile * ROWS)) * DV;
 #pragma unroll
-            for (int t = 0; t < kT; ++t) store_sums(po, w.o[t], t, a.dv, lane);
+            for (int t = 0; t < kT; ++t) store_sums<DV>(po, w.o[t], t, lane);
             if (h == 0) {
                 float* ml = a.part_ml + (job * ROWS + (row - j.tile * ROWS)) * 2;
                 ml[0] = mc;
@@ -237,11 +230,11 @@ __global__ __launch_bounds__(256 * HALVES, ROWS == 128 ? 2 : 1) void full_fwd_ke
         const int64_t at = (j.q_lo + (int64_t)token) * a.H + head;
         const float f = l > 0.0f ? 1.0f / l : 0.0f;
 #pragma unroll
-        for (int t = 0; t < kT; ++t) store_piece<T>(a.out + at * a.dv, w.o[t], t, f, a.dv, lane);
+        for (int t = 0; t < kT; ++t) store_piece<T, DV>(a.out + at * DV, w.o[t], t, f, lane);
         if (h == 0) a.lse[at] = l > 0.0f ? (mc + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
     } else {
         // The four waves' sums of the same rows: to a common reference, added in
-        // LDS [wave][row][D], stored by columns.
+        // LDS [wave][row][DV], stored by columns.
         float* const so = reinterpret_cast<float*>(sh);
         __shared__ float sm[kWaves][32], sl[kWaves][32];
         if (h == 0) {
@@ -255,24 +248,24 @@ __global__ __launch_bounds__(256 * HALVES, ROWS == 128 ? 2 : 1) void full_fwd_ke
         for (int i = 0; i < kWaves; ++i) top = fmaxf(top, sm[i][rw]);
         const float f = mc == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mc - top);
 #pragma unroll
-        for (int t = 0; t < kT; ++t) put_piece<D>(so + wave * 32 * D, w.o[t], t, f, lane);
+        for (int t = 0; t < kT; ++t) put_piece<DV>(so + wave * 32 * DV, w.o[t], t, f, lane);
         wait_and_sync();
-        for (int i = threadIdx.x; i < 32 * (D / 4); i += 256) {
-            const int rr = i / (D / 4), g = i % (D / 4);
+        for (int i = threadIdx.x; i < 32 * (DV / 4); i += 256) {
+            const int rr = i / (DV / 4), g = i % (DV / 4);
             const int32_t rowi = j.tile * ROWS + rr;
-            if (rowi >= nrows || 4 * g >= a.dv) continue;
+            if (rowi >= nrows) continue;
             f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
             float mm = -INFINITY, ll = 0.0f;
 #pragma unroll
             for (int u = 0; u < kWaves; ++u) {
-                x += get_piece<D>(so + u * 32 * D, rr, g);
+                x += get_piece<DV>(so + u * 32 * DV, rr, g);
                 mm = fmaxf(mm, sm[u][rr]);
             }
 #pragma unroll
             for (int u = 0; u < kWaves; ++u)
                 if (sl[u][rr] > 0.0f) ll += sl[u][rr] * __builtin_amdgcn_exp2f(sm[u][rr] - mm);
             if (j.runs > 1) {
-                *reinterpret_cast<f32x4*>(a.part_o + (job * ROWS + rr) * a.dv + 4 * g) = x;
+                *reinterpret_cast<f32x4*>(a.part_o + (job * ROWS + rr) * DV + 4 * g) = x;
                 if (g == 0) {
                     float* ml = a.part_ml + (job * ROWS + rr) * 2;
                     ml[0] = mm;
@@ -282,7 +275,7 @@ __global__ __launch_bounds__(256 * HALVES, ROWS == 128 ? 2 : 1) void full_fwd_ke
             }
             const int64_t at = (j.q_lo + (int64_t)(rowi / a.rep)) * a.H + j.kv_head * a.rep + rowi % a.rep;
             const float inv = ll > 0.0f ? 1.0f / ll : 0.0f;
-            *reinterpret_cast<s16x4*>(a.out + at * a.dv + 4 * g) = round4<T>(x, inv);
+            *reinterpret_cast<s16x4*>(a.out + at * DV + 4 * g) = round4<T>(x, inv);
             if (g == 0) a.lse[at] = ll > 0.0f ? (mm + __builtin_amdgcn_logf(ll)) * kLn2 : -INFINITY;
         }
     }
@@ -363,7 +356,7 @@ __global__ __launch_bounds__(256) void full_join_kernel(const JoinArgs b) {
     }
 }
 
-template <typename T, int D>
+template <typename T, int DK, int DV>
 hipError_t launch_fwd(const FullCall& f, const FullPlan& p, float* part_o, float* part_ml, hipStream_t stream) {
     FwdArgs a{};
     a.q = reinterpret_cast<const char*>(f.q);
@@ -376,7 +369,7 @@ hipError_t launch_fwd(const FullCall& f, const FullPlan& p, float* part_o, float
     a.q_row = 2 * f.q_row, a.q_head = 2 * f.q_head;
     a.k_row = 2 * f.k_row, a.k_head = 2 * f.k_head;
     a.v_row = 2 * f.v_row, a.v_head = 2 * f.v_head;
-    a.H = f.H, a.Hk = f.Hk, a.rep = f.H / f.Hk, a.d = f.d, a.dv = f.dv, a.causal = f.causal != 0;
+    a.H = f.H, a.Hk = f.Hk, a.rep = f.H / f.Hk, a.dv = f.dv, a.causal = f.causal != 0;
     a.split = p.split;
     a.scale = f.scale;
     for (const FullLaunch& l : p.launches) {
@@ -384,11 +377,11 @@ hipError_t launch_fwd(const FullCall& f, const FullPlan& p, float* part_o, float
         a.first_job = l.first_job;
         a.fold = l.fold;
         if (p.rows == 128 && p.halves == 2)
-            hipLaunchKernelGGL((full_fwd_kernel<T, D, 128, 2>), dim3(l.jobs), dim3(512), 0, stream, a);
+            hipLaunchKernelGGL((full_fwd_kernel<T, DK, DV, 128, 2>), dim3(l.jobs), dim3(512), 0, stream, a);
         else if (p.rows == 128)
-            hipLaunchKernelGGL((full_fwd_kernel<T, D, 128, 1>), dim3(l.jobs), dim3(256), 0, stream, a);
+            hipLaunchKernelGGL((full_fwd_kernel<T, DK, DV, 128, 1>), dim3(l.jobs), dim3(256), 0, stream, a);
         else
-            hipLaunchKernelGGL((full_fwd_kernel<T, D, 32, 1>), dim3(l.jobs), dim3(256), 0, stream, a);
+            hipLaunchKernelGGL((full_fwd_kernel<T, DK, DV, 32, 1>), dim3(l.jobs), dim3(256), 0, stream, a);
         hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
         if (l.tile_jobs > 0) {
@@ -413,14 +406,15 @@ hipError_t launch_fwd(const FullCall& f, const FullPlan& p, float* part_o, float
 }  // namespace
 
 hipError_t launch_full_fwd(const FullCall& f, const FullPlan& p, float* part_o, float* part_ml, hipStream_t stream) {
-    const int32_t w = f.d > f.dv ? f.d : f.dv;
-#define KMIP_FULL_FWD(D) \
-    if (w == D) return f.fp16 ? launch_fwd<Fp16, D>(f, p, part_o, part_ml, stream) : launch_fwd<Bf16, D>(f, p, part_o, part_ml, stream);
+#define KMIP_FULL_CASE(DK, DV) \
+    if (f.d == DK && f.dv == DV) return f.fp16 ? launch_fwd<Fp16, DK, DV>(f, p, part_o, part_ml, stream) : launch_fwd<Bf16, DK, DV>(f, p, part_o, part_ml, stream);
+#define KMIP_FULL_FWD(DK) KMIP_FULL_CASE(DK, 16) KMIP_FULL_CASE(DK, 32) KMIP_FULL_CASE(DK, 64) KMIP_FULL_CASE(DK, 128)
     KMIP_FULL_FWD(16)
     KMIP_FULL_FWD(32)
     KMIP_FULL_FWD(64)
     KMIP_FULL_FWD(128)
 #undef KMIP_FULL_FWD
+#undef KMIP_FULL_CASE
     return hipErrorInvalidValue;
 }
 

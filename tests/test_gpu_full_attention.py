@@ -46,6 +46,11 @@ CASES = [
     (BF, 8, 8, 64, 64, [(4097, 4097)], True), (HF, 16, 4, 128, 128, [(700, 1300), (1500, 1500), (1, 9)], True),
     (BF, 16, 16, 32, 32, [(2100, 2100), (33, 129)], False), (BF, 33, 11, 16, 16, [(1000, 1000), (1, 64), (129, 1)], True),
     (HF, 12, 4, 64, 128, [(3000, 2900)], True),
+    # every pair of widths, in both forms
+    *[(BF if i % 2 else HF, 2, 1, d, dv, [(33 + i, 70), (5, 129)], i % 3 == 0)
+      for i, (d, dv) in enumerate((a, b) for a in (16, 32, 64, 128) for b in (16, 32, 64, 128) if a != b)],
+    *[(HF if i % 2 else BF, 16, 8, d, dv, [(1100, 2100), (997, 1200)], i % 3 != 0)
+      for i, (d, dv) in enumerate((a, b) for a in (16, 32, 64, 128) for b in (16, 32, 64, 128))],
     # tiles of 128 rows or keys whose streams are cut into runs
     (BF, 8, 2, 128, 128, [(2048, 4096), (7, 100)], True), (BF, 4, 4, 128, 32, [(3001, 2999)], True),
     (HF, 2, 1, 16, 128, [(5000, 6001)], False), (BF, 6, 2, 32, 32, [(900, 7000), (1, 5), (700, 1100)], True),
