@@ -140,8 +140,8 @@ int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 //     where there are few and long ones: a CU then works on one tile at a time
 //     and the last ones take half as long (8 heads, causal, forward: 8192 tokens,
 //     d = 128 182 us with one group, 165 with two; 16 heads, 4096 tokens, d = 64 65 and 56;
-//     but 4096 tokens of 8 heads at d = 128 91 and 98, 17 prompts of 2000, d = 64 229 and 246, since the groups'
-//     sums have to be added).  width: d + d_V; only_halves: the kernel has only that form.
+//     8 heads, 4096 tokens, d = 128 88 and 71, 12 heads, 3000 tokens, all pairs 87 and 104 (288 tiles: two rounds
+//     on 256 CUs), 17 prompts of 2000, d = 64 229 and 246, since the groups' sums have to be added).  width: d + d_V; only_halves: the kernel has only that form.
 //   32 rows otherwise, in runs of at least 512 where that makes more jobs.
 // Runs cost the sums' way through memory, so that there are as few as fill the chip.
 template <typename Kept, typename Streamed>
@@ -158,11 +158,16 @@ kmip_status_t plan(std::vector<Seq>& seqs, int32_t Hk, bool causal, const Kept& 
     }
     const bool full = 2 * kept >= 128 * jobs;
     p->rows = full && (jobs >= kSlots || work >= kSlots * 512) ? 128 : 32;
-    p->halves = p->rows == 128 && (only_halves || (jobs <= 2 * kSlots && work >= jobs * (width > 192 ? 6144 : 1024))) ? 2 : 1;
+    const int64_t half_slots = kSlots / 2;
+    // jobs >= half_slots run in whole rounds, or shorter ones fill the gaps
+    const bool rounds = jobs >= half_slots && (causal || 4 * jobs >= 3 * round_up(jobs, half_slots));
+    const bool halves = width <= 192 ? jobs <= 2 * kSlots && work >= jobs * 1024
+                                     : (jobs <= 2 * kSlots && work >= jobs * 6144) || (rounds && jobs < kSlots && work >= jobs * 2048);
+    p->halves = p->rows == 128 && (only_halves || halves) ? 2 : 1;
     int64_t run = 0;
     if (p->rows == 32)
         run = std::max<int64_t>(round_up(work32 / (2 * kSlots), 128), 512);
-    else if (jobs < (p->halves == 2 ? kSlots / 2 : kSlots))
+    else if (jobs < (p->halves == 2 ? half_slots : kSlots))
         run = std::max<int64_t>(round_up(work / kSlots, 128), 512);
     static_assert(2 * 512 >= KMIP_FULL_LONG, "streams below are not cut");
     p->split = run > 0 && longest >= 2 * run ? (int32_t)std::min<int64_t>(run, INT32_MAX) : 0;
