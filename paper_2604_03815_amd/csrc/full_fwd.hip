@@ -60,6 +60,10 @@ struct FwdWave {
 #pragma unroll
             for (int t = 0; t < DK / 16; ++t) s[b] = T::mfma(in.x_rows(t, at + b * 64 * DK), q[t], s[b]);
         }
+        // the wave in its exponentials goes first, the other's products run beside them (16 heads, 8192
+        // tokens, d = 64, causal 170 -> 163 us; at wider heads the products are the longer part)
+        constexpr bool kFirst = DK + DV <= 128;
+        if constexpr (kFirst) __builtin_amdgcn_s_setprio(1);
         if (key0 + 32 * NB > lim_first) {
             const int32_t left = lim - key0 - 4 * (lane >> 5);
 #pragma unroll
@@ -98,6 +102,7 @@ struct FwdWave {
                 sum += s[b][r];
             }
             l += sum;
+            if (kFirst && b == NB - 1) __builtin_amdgcn_s_setprio(0);
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 // rounded to the inputs' type, the operand of the product: half a step of each weight
