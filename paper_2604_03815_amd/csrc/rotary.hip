@@ -11,9 +11,14 @@
 // pi/4, goes through the Taylor sums of sine and cosine (to x^9 and x^10:
 // remainders below 2e-9).  All in float32; the row's values are rounded once.
 //
-// A thread takes P pairs of one token for a group of heads, so that an angle is
-// formed once for many heads.  Bound by memory: a row is read once and written
-// once, 16 bytes a lane where the sizes allow.
+// A thread takes P pairs of one token for up to four heads, so that an angle is
+// formed once for them; the threads of a token's heads are neighbours, so that
+// a wave reads and writes whole tokens' rows.  Bound by memory: a row is read
+// once and written once, 16 bytes a lane where the sizes allow.  Cold data, us:
+// 16,383 tokens of 40 heads, d = 128, rot = 64, fp16 70 (4.8 TB/s; 84 where
+// neighbours took other tokens, 92 with a thread for each head, 77 with eight
+// heads a thread), 100,000 of 8 heads, d = 32, float32 to bf16 and back 72 (4.2
+// TB/s; 76, 75 and 89).
 #include <cmath>
 #include <cstring>
 
@@ -34,9 +39,9 @@ struct Side {
 struct RotaryArgs {
     Side s[2];
     const int32_t* positions;
-    uint32_t threads;                 // N * units
-    int32_t units, rot_units;         // threads a token and head group, those with pairs
-    int32_t heads, first_heads, group;
+    uint32_t threads;                 // N * group * units
+    int32_t units, rot_units;         // threads a row, those with pairs
+    int32_t heads, first_heads, group;   // heads of both, of the first, threads that share them
     int32_t rot;
     float cos_scale, sin_scale;
     uint64_t turns[kMostPairs];
@@ -109,7 +114,7 @@ __device__ __forceinline__ void turn(float (&u)[P], float (&v)[P], const float (
     }
 }
 
-// Rows of a thread whose loads go out before the first store (which may write
+// Rows of a thread, whose loads go out before the first store (which may write
 // the same memory, so that the compiler cannot move a load across it).
 constexpr int kRows = 4;
 
@@ -118,8 +123,10 @@ __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs a) {
     constexpr int kIn = sizeof(typename TI::word), kOut = sizeof(typename TO::word);
     const uint32_t id = blockIdx.x * 256u + threadIdx.x;
     if (id >= a.threads) return;
-    const uint32_t token = id / (uint32_t)a.units;
-    const int unit = (int)(id - token * (uint32_t)a.units);
+    const uint32_t place = id / (uint32_t)a.units;
+    const int unit = (int)(id - place * (uint32_t)a.units);
+    const uint32_t token = place / (uint32_t)a.group;
+    const int h0 = (int)(place - token * (uint32_t)a.group);
     const bool turned = unit < a.rot_units;
     // A thread's two runs of P values lie half of the turned (or of the passed
     // on) dimensions apart: neighbouring threads touch neighbouring runs.
@@ -142,24 +149,25 @@ __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs a) {
             s[e] *= a.sin_scale;
         }
     }
-    const int h0 = blockIdx.y * a.group, h1 = min(h0 + a.group, a.heads);
-    for (int h = h0; h < h1; h += kRows) {
+    for (int h = h0; h < a.heads; h += kRows * a.group) {
         Pack<TI, P> x[kRows][2];
 #pragma unroll
         for (int r = 0; r < kRows; ++r) {
-            if (h + r >= h1) break;
-            const bool second = h + r >= a.first_heads;
+            const int hr = h + r * a.group;
+            if (hr >= a.heads) break;
+            const bool second = hr >= a.first_heads;
             const Side& t = a.s[second];
-            const char* p = t.x + (int64_t)token * t.x_row + (second ? h + r - a.first_heads : h + r) * t.x_head;
+            const char* p = t.x + (int64_t)token * t.x_row + (second ? hr - a.first_heads : hr) * t.x_head;
             x[r][0] = *reinterpret_cast<const Pack<TI, P>*>(p + one * kIn);
             x[r][1] = *reinterpret_cast<const Pack<TI, P>*>(p + two * kIn);
         }
 #pragma unroll
         for (int r = 0; r < kRows; ++r) {
-            if (h + r >= h1) break;
-            const bool second = h + r >= a.first_heads;
+            const int hr = h + r * a.group;
+            if (hr >= a.heads) break;
+            const bool second = hr >= a.first_heads;
             const Side& t = a.s[second];
-            char* y = t.y + (int64_t)token * t.y_row + (second ? h + r - a.first_heads : h + r) * t.y_head;
+            char* y = t.y + (int64_t)token * t.y_row + (second ? hr - a.first_heads : hr) * t.y_head;
             float u[P], v[P];
 #pragma unroll
             for (int e = 0; e < P; ++e) u[e] = TI::widen(x[r][0].v[e]), v[e] = TI::widen(x[r][1].v[e]);
@@ -260,24 +268,23 @@ extern "C" kmip_status_t kmip_rotary(const void* X, void* Y, int32_t H, const vo
     a.positions = positions;
     a.units = d / (2 * pairs);
     a.rot_units = rot / 2 / pairs;
-    const int64_t threads = N * a.units;
-    if (threads >= (int64_t(1) << 32) - 256) return record_error(KMIP_ERR_INVALID_ARG, "N * d / %d >= 2^32", 2 * pairs);
-    a.threads = (uint32_t)threads;
     a.heads = H + H2;
     a.first_heads = H;
-    // Heads a thread takes: as many as leave 2^19 threads (32 waves a CU; 16,383
-    // tokens of 40 heads, d = 128, rot = 64: 75 us with 2^18, 73, 76 with 2^20)
-    const int64_t groups = (int64_t(1) << 19) / threads + 1;
-    // Results larger than the chip's 32 MB of L2 are stored past it (the same
-    // tokens 73 -> 71 us; 100,000 of 8 heads, d = 32, float32 to bf16 and back 75 -> 63)
+    // Threads a token and unit: each takes up to kRows heads, one where that leaves
+    // the chip's SIMDs less than two waves (or all, where ids would pass 32 bits)
+    const int64_t runs = N * a.units;
+    a.group = runs * a.heads < (int64_t(1) << 17) ? a.heads : (a.heads + kRows - 1) / kRows;
+    if (runs * a.group >= (int64_t(1) << 32) - 256) a.group = 1;
+    const int64_t threads = runs * a.group;
+    if (threads >= (int64_t(1) << 32) - 256) return record_error(KMIP_ERR_INVALID_ARG, "N * d / %d >= 2^32", 2 * pairs);
+    a.threads = (uint32_t)threads;
+    // Results larger than the chip's 32 MB of L2 are stored past it (100,000 tokens
+    // of 8 heads, d = 32, float32 to bf16 and back 75 us without, 63 with)
     const bool past = pairs > 1 && N * a.heads * d * so > (int64_t(32) << 20);
-    a.group = groups >= a.heads ? 1 : (int32_t)((a.heads + groups - 1) / groups);
-    int32_t ny = (a.heads + a.group - 1) / a.group;
-    if (ny > 65535) a.group = (a.heads + 65534) / 65535, ny = (a.heads + a.group - 1) / a.group;
     a.rot = rot;
     a.cos_scale = magnitude;
     a.sin_scale = inverse ? -magnitude : magnitude;
-    const dim3 grid((unsigned)((threads + 255) / 256), (unsigned)ny);
+    const dim3 grid((unsigned)((threads + 255) / 256));
     const hipStream_t s = reinterpret_cast<hipStream_t>(stream);
     const bool inter = interleaved != 0;
     if (dtype_in == KMIP_BF16) launch_out<Brain16>(a, dtype_out, pairs, inter, past, grid, s);
