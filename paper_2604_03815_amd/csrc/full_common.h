@@ -41,7 +41,10 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
+// The two types.  kUp: the forward's weights are 2^kUp times as large (below
+// 2^15 in float16, whose values below 2^-14 lose bits).
 struct Bf16 {
+    static constexpr float kUp = 0.0f;
     static __device__ __forceinline__ f32x16 mfma(s16x8 a, s16x8 b, f32x16 c) {
         return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0,
                                                        0, 0);
@@ -51,6 +54,7 @@ struct Bf16 {
 };
 
 struct Fp16 {
+    static constexpr float kUp = 7.0f;
     static __device__ __forceinline__ f32x16 mfma(s16x8 a, s16x8 b, f32x16 c) {
         return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0,
                                                       0);

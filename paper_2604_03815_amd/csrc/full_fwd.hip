@@ -79,8 +79,9 @@ struct FwdWave {
             for (int r = 0; r < 16; ++r) top = fmaxf(top, s[b][r]);
         const float2 tops = both_halves(top);
         top = fmaxf(tops.x, tops.y);
-        // The reference follows the maximum only where a weight would pass 2^8: 16-bit
-        // weights keep their relative precision at any reference.
+        // The reference follows the maximum only where a weight would pass 2^8: bfloat16
+        // weights keep their relative precision at any reference; float16 ones are 2^7
+        // times as large (T::kUp), so that small ones have their bits too.
         if (__any((top - m) * c > 8.0f)) {
             const float to = fmaxf(top, m);
             // (no key seen yet: m and top are -inf, and the factor is that of a sum of nothing)
@@ -92,7 +93,7 @@ struct FwdWave {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) o[t][r] *= f;
         }
-        const float mc = m == -INFINITY ? 0.0f : m * c;
+        const float mc = m == -INFINITY ? 0.0f : m * c - T::kUp;
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
             float sum = 0.0f;
@@ -186,7 +187,7 @@ __global__ __launch_bounds__(256 * HALVES, ROWS == 128 ? 2 : 1) void full_fwd_ke
     }
 
     const float2 ls = both_halves(w.l);
-    float l = ls.x + ls.y, mc = w.m == -INFINITY ? -INFINITY : w.m * c;
+    float l = ls.x + ls.y, mc = w.m == -INFINITY ? -INFINITY : w.m * c - T::kUp;
     const int h = lane >> 5;
     if constexpr (HALVES > 1) {
         // the second half's sums to LDS, a piece of 32 columns at a time [wave][piece][4 registers][lane], then added

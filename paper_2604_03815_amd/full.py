@@ -59,8 +59,8 @@ def _new(like, shape, dtype):
 
 
 def _strides(*tensors):
-    """Host int64 pairs of strides."""
-    s = [x for t in tensors for x in t.stride()[:2]]
+    """Host int64 pairs of strides (0 for a dimension of one, whose stride can be anything)."""
+    s = [x if n > 1 else 0 for t in tensors for n, x in zip(t.shape[:2], t.stride())]
     return (ctypes.c_int64 * len(s))(*s)
 
 
@@ -247,7 +247,7 @@ def _full_function():
         def backward(ctx, dout):
             q, k_, v, out, lse = ctx.saved_tensors
             scale, where, workspace = ctx.args
-            if dout.stride(-1) != 1 or any(s % 8 for s in dout.stride()[:2]) or dout.data_ptr() % 16:
+            if dout.stride(-1) != 1 or any(s % 8 for s in dout.stride()[:2]) or dout.stride(0) >= 1 << 23 or dout.data_ptr() % 16:
                 dout = dout.contiguous()
             return (*full_bwd(q, k_, v, dout, out, lse, scale, workspace=workspace, **where), None, None, None)
 

@@ -57,6 +57,42 @@ def test_views(n, heads, d):
         kmip.full_fwd(normal(13, n, heads, d + 4)[:, :, :d], k, v, 1.0)
 
 
+def test_strides_of_single_rows_and_far_gradients():
+    """Strides of dimensions of one do not matter; rows of dout too far apart for the kernels are copied."""
+    q, k, v, g = normal(1, 1, 2, 32), normal(2, 90, 2, 64)[:, :, :32], normal(3, 90, 2, 32), normal(4, 1, 2, 32)
+    q = torch.as_strided(q, (1, 2, 32), (7, 32, 1))
+    got, want = both(q, k, v, g, 0.2), both(q.contiguous(), k.contiguous(), v, g, 0.2)
+    for name in got:
+        assert torch.equal(got[name], want[name]), name
+    q, k, v = (normal(s, 3, 2, 32).requires_grad_() for s in (5, 6, 7))
+    far = torch.zeros(3, 1 << 23, dtype=BF, device="cuda")
+    far[:, :64] = normal(8, 3, 64)
+    g = far[:, :64].view(3, 2, 32)
+    out = kmip.full_attention(q, k, v, 0.2)
+    for x, y in zip(torch.autograd.grad(out, (q, k, v), g, retain_graph=True), torch.autograd.grad(out, (q, k, v), g.contiguous())):
+        assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("m", [1, 300])
+def test_small_float16_weights(m):
+    """One key outweighs each other one by e^12.2 and has value 0: the result is the sum of 4,000 like, small weights."""
+    n, d = 4001, 16
+    q, k, v = (torch.zeros(*s, 1, d, dtype=HF, device="cuda") for s in ((m,), (n,), (n,)))
+    q[..., 0] = 1.0
+    k[..., 0] = 0.3
+    k[0, 0, 0] = 12.5
+    v[1:] = 4096.0
+    out, lse = kmip.full_fwd(q, k, v, 1.0)
+    s = k[:, 0, 0].double()
+    want = torch.softmax(s, 0)[1:].sum() * 4096.0
+    # every weight off by half a step of its own (2^-11), the result by another; n additions in 32 bits, for the sum and
+    # its normaliser, by at most 2^-24 each; scores and exponentials by 2^-20.  (A weight of e^-12.2 among float16's
+    # subnormal numbers, 2^-24 apart, would be off by 0.5 %.)
+    bound = want * (2.0 ** -10 + 2 * n * 2.0 ** -24 + 2.0 ** -20)
+    assert ((out.double() - want).abs() <= bound).all()
+    assert (lse.double() - torch.logsumexp(s, 0)).abs().max() <= 2.0 ** -18
+
+
 @pytest.mark.parametrize("heads,kv,d,dv,causal", [(8, 2, 64, 64, True), (3, 3, 16, 32, False), (4, 1, 128, 128, True)])
 def test_cache_with_room(heads, kv, d, dv, causal):
     """Rows behind a slot's keys in use are not read (NaN there) and get gradient 0; nothing beside the outputs is written."""
