@@ -129,18 +129,12 @@ __global__ __launch_bounds__(256 * HALVES, ROWS == 128 ? 2 : 1) void full_dq_ker
     if constexpr (ROWS == 128) {
         const int32_t n = lo < hi ? (hi - lo - 1) / kTile + 1 : 0, most = (n + HALVES - 1) / HALVES;
         const int32_t first = lo + half * most * kTile, mine = half == 0 ? most : n - most;
-        if (mine > 0) fetch(first, 0);
-        auto stage = [&](int32_t i, auto buf) {
-            const int32_t key = first + i * kTile;
-            wait_and_sync();
-            if (i + 1 < mine) fetch(key + kTile, buf ^ 1);
-            if (i < mine && key < lim_last)
-                compute(key, Constant<decltype(buf)::value * B::kBytes>());
-        };
-        for (int32_t i = 0; i < most; i += 2) {
-            stage(i, std::integral_constant<int, 0>());
-            if (i + 1 < most) stage(i + 1, std::integral_constant<int, 1>());
-        }
+        stream_tiles(
+            most, mine, [&](int32_t i, int buf) { fetch(first + i * kTile, buf); },
+            [&](int32_t i, auto buf) {
+                const int32_t key = first + i * kTile;
+                if (key < lim_last) compute(key, Constant<decltype(buf)::value * B::kBytes>());
+            });
         if constexpr (HALVES > 1)
             if (!add_half<kT>(acc, sh, wave, half, lane)) return;
         if (!live) return;
@@ -236,6 +230,7 @@ __global__ __launch_bounds__(256 * HALVES, KEYS == 128 ? 2 : 1) void full_dkv_ke
     PairLoad<B, DK, DV, KEYS == 128> load;
     load.init(lane, wave, a.q_row, a.do_row);
     const uint32_t st_base = lds_addr(stats);
+    const int64_t to_D = a.D - a.lse2;   // (both lie in the workspace)
     auto fetch = [&](int32_t hr, int32_t tok, int buf) {
         const int32_t head = kv_head * a.rep + hr;
         load.issue(base + buf * B::kBytes, a.q + (q_lo + (int64_t)tok) * a.q_row + head * a.q_head,
@@ -244,7 +239,7 @@ __global__ __launch_bounds__(256 * HALVES, KEYS == 128 ? 2 : 1) void full_dkv_ke
         if (part < kTile / 32) {
             const int i = 64 * part + lane;
             const int64_t at = (q_lo + (int64_t)min(tok + i % kTile, q_len - 1)) * a.H + head;
-            load_word_to_lds(st_base + buf * kTile * 8 + 256 * part, (i < kTile ? a.lse2 : a.D) + at);
+            load_word_to_lds(st_base + buf * kTile * 8 + 256 * part, a.lse2 + at + (i < kTile ? 0 : to_D));
         }
     };
     PairOperands<B, DK, DV> in;
@@ -311,27 +306,20 @@ __global__ __launch_bounds__(256 * HALVES, KEYS == 128 ? 2 : 1) void full_dkv_ke
     const int64_t job = (int64_t)a.first_job + blockIdx.x;
     if constexpr (KEYS == 128) {
         const int32_t most = (n + HALVES - 1) / HALVES, mine = half == 0 ? most : n - most, begin = first + half * most;
-        int32_t hr = 0, tok = 0;   // of the tile that is fetched next
-        if (mine > 0) {
-            hr = begin / per;
-            tok = t_lo + begin % per * kTile;
-            fetch(hr, tok, 0);
-        }
-        auto stage = [&](int32_t i, auto buf) {
-            const int32_t now = tok;
-            wait_and_sync();
-            if (i + 1 < mine) {
-                tok += kTile;
-                if (tok >= q_len) tok = t_lo, ++hr;
-                fetch(hr, tok, buf ^ 1);
-            }
-            if (i < mine && now + kTile > t_wave)
-                compute(now, Constant<decltype(buf)::value * B::kBytes>(), decltype(buf)::value);
-        };
-        for (int32_t i = 0; i < most; i += 2) {
-            stage(i, std::integral_constant<int, 0>());
-            if (i + 1 < most) stage(i + 1, std::integral_constant<int, 1>());
-        }
+        const int32_t tok0 = mine > 0 ? t_lo + begin % per * kTile : 0;
+        int32_t hr = mine > 0 ? begin / per : 0, tok = tok0, now = tok0;   // of the tile that is fetched next, of the one in use
+        auto next = [&](int32_t t) { return t + kTile < q_len ? t + kTile : t_lo; };
+        stream_tiles(
+            most, mine,
+            [&](int32_t, int buf) {
+                fetch(hr, tok, buf);
+                tok = next(tok);
+                hr += tok == t_lo;
+            },
+            [&](int32_t, auto buf) {
+                if (now + kTile > t_wave) compute(now, Constant<decltype(buf)::value * B::kBytes>(), decltype(buf)::value);
+                now = next(now);
+            });
         if constexpr (HALVES > 1) {
             add_half<kTK>(dk, sh, wave, half, lane);
             if (!add_half<kTV>(dv, sh, wave, half, lane)) return;

@@ -26,6 +26,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "kmip_device.h"
 #include "full_plan.h"
 
@@ -127,15 +129,33 @@ __device__ __forceinline__ float2 both_halves(float x) {
     return make_float2(__uint_as_float(p[0]), __uint_as_float(p[1]));
 }
 
+// x, uniform over the wave, in scalar registers.
+__device__ __forceinline__ uint32_t uniform(uint32_t x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ uint64_t uniform(uint64_t x) { return (uint64_t)uniform((uint32_t)(x >> 32)) << 32 | uniform((uint32_t)x); }
+
 // Memory to LDS, 16 bytes a lane: lane l's 16 bytes at base + off go to
-// lds + 16 l (base and lds uniform).
+// lds + 16 l (base and lds uniform; the LDS address travels in m0, which is left
+// as it was).  No register is written, and the kernels wait by count (wait_loads
+// and what follows): with the compiler's own form of these loads, it waits for
+// all of them before any transposed read of LDS, which holds up every tile's
+// second product until the next tile has arrived.  (Waits of the instructions:
+// one between m0 and the load, five between a vector instruction that wrote base
+// and the load.)
 __device__ __forceinline__ void load_to_lds(uint32_t lds, const char* base, uint32_t off) {
-    __builtin_amdgcn_global_load_lds((const KMIP_GLOBAL void*)(base + off), (KMIP_LDS void*)(uintptr_t)lds, 16, 0, 0);
+    uint32_t m0;
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %2, %3\n\ts_mov_b32 m0, %0"
+                 : "=&s"(m0)
+                 : "s"(uniform(lds)), "v"(off), "s"(uniform((uint64_t)base))
+                 : "memory");
 }
 
 // The same with 4 bytes a lane, each from an address of its own.
 __device__ __forceinline__ void load_word_to_lds(uint32_t lds, const float* p) {
-    __builtin_amdgcn_global_load_lds((const KMIP_GLOBAL void*)p, (KMIP_LDS void*)(uintptr_t)lds, 4, 0, 0);
+    uint32_t m0;
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %2, off\n\ts_mov_b32 m0, %0"
+                 : "=&s"(m0)
+                 : "s"(uniform(lds)), "v"(p)
+                 : "memory");
 }
 
 // All but the last n loads of this wave have ended.
@@ -143,6 +163,11 @@ template <int N>
 __device__ __forceinline__ void wait_loads() {
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
+
+// All loads of this wave have ended, those to registers among them, in a form
+// that the compiler knows (it would wait for them where they are used, in the
+// loop, and there for all loads to LDS too).
+__device__ __forceinline__ void wait_all_loads() { __builtin_amdgcn_s_waitcnt(0x0F70); }
 
 // All LDS accesses of this wave have ended.
 __device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
@@ -347,6 +372,24 @@ struct PairLoad {
     }
 };
 
+// A group of waves' stream of `mine` tiles through two buffers, in step with another group's of at most `most`:
+// `fetch(i, buf)` issues this wave's loads of tile i, `use(i, buf)` computes on it.  One barrier a tile.  (A third
+// buffer and loads two tiles ahead changed nothing: 64 texts of up to 1000 tokens, d = 64 197 and 199 us.)
+template <typename Fetch, typename Use>
+__device__ __forceinline__ void stream_tiles(int32_t most, int32_t mine, const Fetch& fetch, const Use& use) {
+    auto stage = [&](int32_t i, auto buf) {
+        wait_and_sync();
+        if (i + 1 < mine) fetch(i + 1, buf ^ 1);
+        if (i < mine) use(i, buf);
+    };
+    if (mine > 0) fetch(0, 0);
+    wait_all_loads();
+    for (int32_t i = 0; i < most; i += 2) {
+        stage(i, std::integral_constant<int, 0>());
+        if (i + 1 < most) stage(i + 1, std::integral_constant<int, 1>());
+    }
+}
+
 // A wave's own stream: `fetch(i, stage)` issues block i's loads (LOADS
 // instructions), `use(i, stage)` computes on it, for i < n.
 template <int STAGES, int LOADS, typename Fetch, typename Use>
@@ -355,6 +398,7 @@ __device__ __forceinline__ void stream_blocks(int32_t n, const Fetch& fetch, con
 #pragma unroll
     for (int i = 0; i < STAGES - 1; ++i)
         if (i < n) fetch(i, i);
+    wait_all_loads();
     for (int32_t i = 0, stage = 0; i < n; ++i, stage = stage + 1 == STAGES ? 0 : stage + 1) {
         if (i + STAGES - 1 < n) {
             wait_lds();   // the reads of the stage that is filled again

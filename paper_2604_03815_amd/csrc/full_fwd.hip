@@ -164,18 +164,13 @@ __global__ __launch_bounds__(256 * HALVES, ROWS == 128 ? 2 : 1) void full_fwd_ke
         // each half takes its part of the tiles; the first one's is as long or one longer
         const int32_t n = lo < hi ? (hi - lo - 1) / kTile + 1 : 0, most = (n + HALVES - 1) / HALVES;
         const int32_t first = lo + half * most * kTile, mine = half == 0 ? most : n - most;
-        if (mine > 0) fetch(first, 0);
-        auto stage = [&](int32_t i, auto buf) {
-            const int32_t key = first + i * kTile;
-            wait_and_sync();
-            if (i + 1 < mine) fetch(key + kTile, buf ^ 1);
-            if (i < mine && key < lim_last)
-                w.template step<kTile / 32>(in, Constant<decltype(buf)::value * B::kBytes>(), key, lim_first, c, lane);
-        };
-        for (int32_t i = 0; i < most; i += 2) {
-            stage(i, std::integral_constant<int, 0>());
-            if (i + 1 < most) stage(i + 1, std::integral_constant<int, 1>());
-        }
+        stream_tiles(
+            most, mine, [&](int32_t i, int buf) { fetch(first + i * kTile, buf); },
+            [&](int32_t i, auto buf) {
+                const int32_t key = first + i * kTile;
+                if (key < lim_last)
+                    w.template step<kTile / 32>(in, Constant<decltype(buf)::value * B::kBytes>(), key, lim_first, c, lane);
+            });
     } else {
         // blocks lo + 32 (wave + 4 i)
         const int32_t mine = lo + 32 * wave, n = mine < hi ? (hi - mine + 32 * kWaves - 1) / (32 * kWaves) : 0;
