@@ -133,17 +133,26 @@ constexpr int64_t kSlots = 512;   // workgroups resident at once, two on each of
 int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
 // How `seqs` become tiles of kept rows, kept_of(s) of them for each key head, that
-// stream streamed_of(s) rows each.
+// stream streamed_of(s) rows each; width: d + d_V.
 //   128 rows: waves share the streamed tiles, a quarter of the traffic; for
 //     tiles that are at least half full and fill the chip, by themselves or in runs
-//     of at least 512 streamed rows.  With two groups of waves on a tile (halves)
-//     where there are few and long ones: a CU then works on one tile at a time
-//     and the last ones take half as long (8 heads, causal, forward: 8192 tokens,
-//     d = 128 182 us with one group, 165 with two; 16 heads, 4096 tokens, d = 64 65 and 56;
-//     8 heads, 4096 tokens, d = 128 88 and 71, 12 heads, 3000 tokens, all pairs 87 and 104 (288 tiles: two rounds
-//     on 256 CUs), 17 prompts of 2000, d = 64 229 and 246, since the groups' sums have to be added).  width: d + d_V; only_halves: the kernel has only that form.
-//   32 rows otherwise, in runs of at least 512 where that makes more jobs.
+//     of at least 512 streamed rows.
+//   32 rows otherwise, in runs of at least 512 where that makes more jobs (one text
+//     of 1000 tokens, 8 heads, d = 64, forward and backward 40 us; 64 such texts of up to 1000
+//     329 with this form, 196 with the other).
 // Runs cost the sums' way through memory, so that there are as few as fill the chip.
+//
+// Two groups of waves on a 128-row tile (halves; only_halves: the kernel has no
+// other form): a CU works on one tile at a time and the last ones take half as
+// long, but the groups' sums have to be added and fewer workgroups share a CU.
+// So where there are few jobs and they are long; up to a whole round of CUs earlier than
+// with more, and at narrow widths, whose sums are small, too.  us with one group and with two:
+//   d = 32, causal, forward and backward: 16 heads, 3000 tokens 119, 103; 4 texts of 2048, 8 heads 115, 105
+//   d = 64, the same: 8 heads, 4 texts of up to 2000 (208 jobs) 104, 77; 16 heads, 3000 tokens (376) 173, 159,
+//     4096 tokens (512) 238, 206; 8 heads, 8 texts of up to 2000 (800 jobs of 1500 rows) 156, 169;
+//     all pairs, 8 graphs of 1024 (512 jobs) 99, 108
+//   d = 128, 8 heads, causal, forward: 8192 tokens 182, 165; 4096 tokens 88, 71; 12 heads, 3000 tokens, all
+//     pairs 87, 104 (288 tiles: two rounds on 256 CUs)
 template <typename Kept, typename Streamed>
 kmip_status_t plan(std::vector<Seq>& seqs, int32_t Hk, bool causal, const Kept& kept_of, const Streamed& streamed_of, int32_t width, bool only_halves,
                    FullPlan* p) {
@@ -161,7 +170,8 @@ kmip_status_t plan(std::vector<Seq>& seqs, int32_t Hk, bool causal, const Kept& 
     const int64_t half_slots = kSlots / 2;
     // jobs >= half_slots run in whole rounds, or shorter ones fill the gaps
     const bool rounds = jobs >= half_slots && (causal || 4 * jobs >= 3 * round_up(jobs, half_slots));
-    const bool halves = width <= 192 ? jobs <= 2 * kSlots && work >= jobs * 1024
+    const int64_t least = width <= 64 || jobs <= half_slots ? 1024 : 2048;
+    const bool halves = width <= 192 ? jobs <= 2 * kSlots && work >= jobs * least
                                      : (jobs <= 2 * kSlots && work >= jobs * 6144) || (rounds && jobs < kSlots && work >= jobs * 2048);
     p->halves = p->rows == 128 && (only_halves || halves) ? 2 : 1;
     int64_t run = 0;
@@ -190,6 +200,9 @@ kmip_status_t plan_keys(const Sequences& sq, int32_t H, int32_t Hk, bool causal,
         if (sq.at(g).k_slot > 0) seqs.push_back(sq.at(g));
     return plan(seqs, Hk, causal, [](const Seq& s) { return (int64_t)s.k_slot; }, [=](const Seq& s) { return s.q_len * rep; }, width, width == 256, p);
 }
+
+// (The workspace queries plan without a mask: a causal plan never has more runs, since a mask only makes two groups, and so
+// none or longer ones, more likely.)
 
 // Workspace of the forward: the runs' sums, then their maxima and sums of weights.
 struct FwdLayout {

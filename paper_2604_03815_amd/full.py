@@ -223,7 +223,9 @@ def full_attention(q, k_, v, scale: float, graph_offsets: Optional[Sequence[int]
     """Differentiable full softmax attention: returns out [Nq, H, dv] of the inputs' type.
 
     The forward is ``full_fwd``; autograd's backward calls ``full_bwd`` with
-    the saved out and lse.  Once differentiable.
+    the saved out and lse.  Once differentiable.  To capture a backward into a
+    HIP graph, run it on a side stream first, and let go of every eager result of
+    the same leaves: autograd ties a leaf's gradient to the stream of the first.
     """
     # (copies: the caller may change its own before the backward)
     where = {n: None if x is None else np.array(x) for n, x in (("graph_offsets", graph_offsets), ("key_offsets", key_offsets),
