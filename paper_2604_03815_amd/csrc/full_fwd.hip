@@ -15,12 +15,27 @@
 //
 // Two forms:
 //   ROWS = 128: four waves of 32 rows share each tile of keys (two buffers,
-//     one barrier a tile);
+//     one barrier a tile); with HALVES = 2 two such groups, each on half of
+//     the tiles, whose sums are added at the end;
 //   ROWS = 32: the four waves hold the same rows and take every fourth block of
 //     32 keys, each with LDS of its own and no barrier, and are joined at the
 //     end.  For few rows.
 // With `split` keys per job, jobs of a row tile take runs of its keys and write
 // partial sums, which full_join_kernel joins in the order of the runs.
+//
+// Measured (MI355X) and what bounds it:
+//   - d = 128: matrix and vector instructions, which overlap in part, and power
+//     (2.0 to 2.2 GHz).  A prompt of 16,384 tokens, 8 heads on 2 key heads, causal: 538
+//     us, 1.02 PFLOP/s (a library product of 8192^3: 1.2); the matrix units are busy 48% of the
+//     time, the vector units issue 40% of it.  Interleaving the scores of a
+//     tile, the weights of the one before and the product of the one before that
+//     in one block of code gave nothing (580 us for 584 then).
+//   - d <= 64: vector issue.  64 keys of 32 rows at d = 64 are 98 vector
+//     instructions, 32 exponentials and 16 products: 1014 clocks if nothing
+//     waits, 1219 measured (17 prompts of up to 4000 tokens, 16 heads on 4, 215 us).
+//   - few rows: the cache's bytes.  One token over each of 64 caches of up to 32,767,
+//     32 heads on 8, d = 128: 203 us, 5.5 TB/s (a large copy moves 4.9, reads alone
+//     5.3 to 6.5), and 6 us for the join.
 #include <type_traits>
 
 #include "full_common.h"
@@ -119,7 +134,7 @@ template <typename T, int DK, int DV, int ROWS, int HALVES>
 __global__ __launch_bounds__(256 * HALVES, ROWS == 128 ? 2 : 1) void full_fwd_kernel(const FwdArgs a) {
     using B = Buffers<DK, DV, ROWS == 128 ? (DK + DV == 32 ? 128 : 64) : 32>;   // [buffer][K, V]
     constexpr int kTile = B::kTile, kWaves = 4, kOwn = ROWS == 128 ? HALVES : kWaves;   // buffer sets
-    constexpr int kBufs = ROWS == 128 ? 2 : B::kOwnStages, kT = kPieces<DV>;
+    constexpr int kBufs = 2, kT = kPieces<DV>;
     __shared__ __attribute__((aligned(1024))) char sh[kOwn * kBufs * B::kBytes];
     static_assert(ROWS == 128 || sizeof(sh) >= 32 * DV * 4 * kWaves, "room for the join");
 
@@ -289,7 +304,7 @@ struct JoinArgs {
     int32_t lanes;              // threads that share a row's four columns, a power of two
 };
 
-// Joins the runs of row tiles.  A thread takes four columns of a row and every
+// Joins the runs of row tiles (5 to 6 us, latency).  A thread takes four columns of a row and every
 // lanes-th run in one pass (reference, sum of weights, sums), then the threads
 // of a row are joined in their order.
 template <typename T>
