@@ -92,16 +92,22 @@ kmip_status_t cut(std::vector<Seq>& seqs, bool causal, const Tiles& tiles_of, co
     auto cost = [](const Seq& s) { return (int64_t)std::max(s.q_len, 1) * std::max(s.k_len, 1); };
     std::stable_sort(seqs.begin(), seqs.end(), [&](const Seq& x, const Seq& y) { return cost(x) > cost(y); });
     p->jobs = 0;
-    for (size_t first = 0; first < seqs.size(); first += kmip::kFullSeqs) {
+    // (a call with runs keeps the long form, whose launches list the cut sequences a second time)
+    bool same = p->split == 0;
+    for (const Seq& s : seqs) same = same && s.q_lo == s.k_lo && s.q_len == s.k_len && s.k_len == s.k_slot;
+    const size_t most = same ? 2 * kmip::kFullSeqs : kmip::kFullSeqs;
+    for (size_t first = 0; first < seqs.size(); first += most) {
         p->launches.emplace_back();
         FullLaunch& l = p->launches.back();
         std::memset(static_cast<void*>(&l), 0, sizeof(l));
-        const size_t n = std::min(seqs.size() - first, (size_t)kmip::kFullSeqs);
+        const size_t n = std::min(seqs.size() - first, most);
+        l.seqs.same = same;
         int64_t jobs = 0, tile_jobs = 0;
-        auto put = [](kmip::FullSeqs& q, const Seq& s, int64_t job0) {
+        auto put = [&](kmip::FullSeqs& q, const Seq& s, int64_t job0) {
             const int32_t i = q.count++;
-            q.q_lo[i] = s.q_lo, q.q_len[i] = s.q_len, q.k_lo[i] = s.k_lo, q.k_len[i] = s.k_len, q.k_slot[i] = s.k_slot;
-            q.job0[i] = (int32_t)job0;
+            int32_t* const w = q.w + i;
+            w[0] = s.q_lo, w[most] = s.q_len, w[2 * most] = (int32_t)job0;
+            if (!same) w[3 * most] = s.k_lo, w[4 * most] = s.k_len, w[5 * most] = s.k_slot;
             return i;
         };
         for (size_t i = 0; i < n; ++i) {

@@ -223,9 +223,13 @@ struct TileLoad {
 // The sequence a job belongs to (uniform over the workgroup).
 __device__ __forceinline__ int seq_of_job(const FullSeqs& s, int32_t job, int lane) {
     int n = 0;
+    auto add = [&](int i) { n += __popcll(__ballot(i + lane < s.count && s.job0(i + lane) <= job)); };
 #pragma unroll
-    for (int i = 0; i < kFullSeqs; i += 64)
-        n += __popcll(__ballot(i + lane < s.count && s.job0[i + lane] <= job));
+    for (int i = 0; i < kFullSeqs; i += 64) add(i);
+    if (s.same) {
+#pragma unroll
+        for (int i = kFullSeqs; i < 2 * kFullSeqs; i += 64) add(i);
+    }
     return n - 1;
 }
 
@@ -240,15 +244,15 @@ __device__ __forceinline__ RowJob row_job(const FullSeqs& seqs, int32_t Hk, int3
                                           int32_t job, int lane) {
     const int s = __builtin_amdgcn_readfirstlane(seq_of_job(seqs, job, lane));
     RowJob j;
-    j.q_lo = seqs.q_lo[s];
-    j.q_len = seqs.q_len[s];
-    j.k_lo = seqs.k_lo[s];
-    j.k_len = seqs.k_len[s];
+    j.q_lo = seqs.q_lo(s);
+    j.q_len = seqs.q_len(s);
+    j.k_lo = seqs.k_lo(s);
+    j.k_len = seqs.k_len(s);
     j.runs = full_runs(j.k_len, split);
     const int32_t tiles = (int32_t)(((int64_t)j.q_len * rep + ROWS - 1) / ROWS);
     // key heads first: with 8 of them (or a divisor) workgroups of one XCD,
     // which come round robin, share a head's keys in its L2
-    int32_t rest = job - seqs.job0[s];
+    int32_t rest = job - seqs.job0(s);
     j.kv_head = rest % Hk;
     rest /= Hk;
     j.run = rest % j.runs;

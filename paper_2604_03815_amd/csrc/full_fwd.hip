@@ -313,8 +313,8 @@ __global__ __launch_bounds__(256) void full_join_kernel(const JoinArgs b) {
     __shared__ f32x4 part[256];
     __shared__ float sm[256], sl[256];
     const int s = __builtin_amdgcn_readfirstlane(seq_of_job(a.s, blockIdx.x, threadIdx.x & 63));
-    const int32_t q_lo = a.s.q_lo[s], nrows = a.s.q_len[s] * a.rep, runs = full_runs(a.s.k_len[s], a.split);
-    const int32_t tiles = (nrows - 1) / b.rows + 1, kv_head = (blockIdx.x - a.s.job0[s]) % a.Hk, place = (blockIdx.x - a.s.job0[s]) / a.Hk;
+    const int32_t q_lo = a.s.q_lo(s), nrows = a.s.q_len(s) * a.rep, runs = full_runs(a.s.k_len(s), a.split);
+    const int32_t tiles = (nrows - 1) / b.rows + 1, kv_head = (blockIdx.x - a.s.job0(s)) % a.Hk, place = (blockIdx.x - a.s.job0(s)) / a.Hk;
     const int32_t tile = full_tile(place, tiles, a.causal, false, a.fold);
     const int groups = a.dv / 4, at_once = 256 / groups / b.lanes;
     const int g = threadIdx.x % groups, t = threadIdx.x / groups % b.lanes;

@@ -168,6 +168,21 @@ def test_many_sequences():
     against64(both(q, k, v, g, 0.25, True, **where), q, k, v, g, 0.25, True, **where)
 
 
+@pytest.mark.parametrize("n,causal", [(256, False), (257, True), (600, False)])
+def test_many_graphs(n, causal):
+    """As many graphs as one launch takes where queries and keys lie alike, one more, and many; empty ones among them."""
+    ql = np.random.default_rng(n).integers(0, 30, n).tolist()
+    ql[5], ql[n - 1] = 0, 150
+    where = dict(graph_offsets=sums(ql))
+    q, k, v, g = (normal(s, sum(ql), h, 16) for s, h in ((1, 2), (2, 1), (3, 1), (4, 2)))
+    got = both(q, k, v, g, 0.25, causal, **where)
+    against64(got, q, k, v, g, 0.25, causal, **where)
+    if not causal:   # the same with the offsets of the keys given
+        again = both(q, k, v, g, 0.25, causal, key_offsets=list(where["graph_offsets"]), **where)
+        for name in got:
+            assert torch.equal(got[name], again[name]), name
+
+
 def test_offsets_past_32_bits():
     """A sequence at the end of a cache of more than 4 GB, and its gradients."""
     nk, n, m, d = (1 << 24) + 5000, 333, 40, 128
