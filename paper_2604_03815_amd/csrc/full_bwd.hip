@@ -200,11 +200,11 @@ __global__ __launch_bounds__(256 * HALVES, KEYS == 128 ? 2 : 1) void full_dkv_ke
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6 & 3);
     const int half = HALVES > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 8) : 0;
-    const int sq = __builtin_amdgcn_readfirstlane(seq_of_job(a.s, blockIdx.x, lane));
-    const int32_t q_lo = a.s.q_lo(sq), q_len = a.s.q_len(sq), k_lo = a.s.k_lo(sq), k_len = a.s.k_len(sq), slot = a.s.k_slot(sq);
-    const int32_t runs = full_runs((int64_t)q_len * a.rep, a.split), kv_head = (blockIdx.x - a.s.job0(sq)) % a.Hk;
-    const int32_t rest = (blockIdx.x - a.s.job0(sq)) / a.Hk, run = rest % runs;
-    const int32_t tile = full_tile(rest / runs, (slot - 1) / KEYS + 1, a.causal, true, a.fold);
+    const JobSeq sq = seq_of_job(a.s, blockIdx.x, lane);
+    const int32_t q_lo = sq.q_lo, q_len = sq.q_len, k_lo = sq.k_lo, k_len = sq.k_len, slot = sq.k_slot;
+    const int32_t runs = full_runs((int64_t)q_len * a.rep, a.split), kv_head = (blockIdx.x - sq.job0) % a.Hk;
+    const int32_t rest = (blockIdx.x - sq.job0) / a.Hk, run = runs > 1 ? rest % runs : 0;
+    const int32_t tile = full_tile(runs > 1 ? rest / runs : rest, (slot - 1) / KEYS + 1, a.causal, true, a.fold);
     const int32_t off = k_len - q_len;
     const int32_t tile_lo = tile * KEYS;                       // keys from here on
     const int32_t key0 = tile_lo + (KEYS == 128 ? 32 * wave : 0), key = key0 + (lane & 31);
@@ -404,22 +404,22 @@ struct SumArgs {
 // Adds the runs of a tile in their order.
 template <typename T>
 __global__ __launch_bounds__(256) void full_sum_kernel(const SumArgs a) {
-    const int s = __builtin_amdgcn_readfirstlane(seq_of_job(a.s, blockIdx.x, threadIdx.x & 63));
-    const int32_t nrows = a.keys ? a.s.k_slot(s) : a.s.q_len(s) * a.rep;
-    const int32_t runs = full_runs(a.keys ? (int64_t)a.s.q_len(s) * a.rep : a.s.k_len(s), a.split);
-    const int32_t kv_head = (blockIdx.x - a.s.job0(s)) % a.Hk, place = (blockIdx.x - a.s.job0(s)) / a.Hk;
+    const JobSeq s = seq_of_job(a.s, blockIdx.x, threadIdx.x & 63);
+    const int32_t nrows = a.keys ? s.k_slot : s.q_len * a.rep;
+    const int32_t runs = full_runs(a.keys ? (int64_t)s.q_len * a.rep : s.k_len, a.split);
+    const int32_t kv_head = (blockIdx.x - s.job0) % a.Hk, place = (blockIdx.x - s.job0) / a.Hk;
     const int32_t tile = full_tile(place, (nrows - 1) / a.rows + 1, a.causal, a.keys, a.fold);
     const int which = blockIdx.z, width = a.width[which], groups = width / 4;
     const int i = blockIdx.y * 256 + threadIdx.x, rr = i / groups, g = i % groups;
     const int32_t row = tile * a.rows + rr;
     if (rr >= a.rows || row >= nrows) return;
-    const float* p = a.part[which] + (((int64_t)a.first_job + a.part0[s] + (int64_t)place * runs * a.Hk + kv_head) * a.rows + rr) * width + 4 * g;
+    const float* p = a.part[which] + (((int64_t)a.first_job + a.part0[s.index] + (int64_t)place * runs * a.Hk + kv_head) * a.rows + rr) * width + 4 * g;
     const int64_t step = (int64_t)a.Hk * a.rows * width;
     f32x4 x = *reinterpret_cast<const f32x4*>(p);
 #pragma unroll 4
     for (int32_t r = 1; r < runs; ++r) x += *reinterpret_cast<const f32x4*>(p + r * step);
-    const int64_t at = a.keys ? (a.s.k_lo(s) + (int64_t)row) * a.Hk + kv_head
-                              : (a.s.q_lo(s) + (int64_t)(row / a.rep)) * (a.Hk * a.rep) + kv_head * a.rep + row % a.rep;
+    const int64_t at = a.keys ? (s.k_lo + (int64_t)row) * a.Hk + kv_head
+                              : (s.q_lo + (int64_t)(row / a.rep)) * (a.Hk * a.rep) + kv_head * a.rep + row % a.rep;
     *reinterpret_cast<s16x4*>(a.to[which] + at * width + 4 * g) = round4<T>(x, a.scale[which]);
 }
 

@@ -221,16 +221,33 @@ struct TileLoad {
 // ---- jobs (full_plan.h) ----
 
 // The sequence a job belongs to (uniform over the workgroup).
-__device__ __forceinline__ int seq_of_job(const FullSeqs& s, int32_t job, int lane) {
+struct JobSeq {
+    int32_t index, q_lo, q_len, job0, k_lo, k_len, k_slot;
+};
+
+// Lanes take entries; what they hold of the found one is read from its lane, so
+// that the search and the entry cost one trip to the arguments and not two.
+__device__ __forceinline__ JobSeq seq_of_job(const FullSeqs& s, int32_t job, int lane) {
+    if (s.count == 1) return JobSeq{0, s.q_lo(0), s.q_len(0), s.job0(0), s.k_lo(0), s.k_len(0), s.k_slot(0)};
+    JobSeq j{};
     int n = 0;
-    auto add = [&](int i) { n += __popcll(__ballot(i + lane < s.count && s.job0(i + lane) <= job)); };
-#pragma unroll
-    for (int i = 0; i < kFullSeqs; i += 64) add(i);
-    if (s.same) {
-#pragma unroll
-        for (int i = kFullSeqs; i < 2 * kFullSeqs; i += 64) add(i);
+    for (int i = 0; i < s.count; i += 64) {
+        const int e = i + lane < s.count ? i + lane : s.count - 1;
+        const int32_t q_lo = s.q_lo(e), q_len = s.q_len(e), job0 = s.job0(e), k_lo = s.k_lo(e), k_len = s.k_len(e), k_slot = s.k_slot(e);
+        const int here = __popcll(__ballot(i + lane < s.count && job0 <= job));
+        if (here == 0) break;
+        n = i + here;
+        const int l = here - 1;
+        j = JobSeq{n - 1,
+                   __builtin_amdgcn_readlane(q_lo, l),
+                   __builtin_amdgcn_readlane(q_len, l),
+                   __builtin_amdgcn_readlane(job0, l),
+                   __builtin_amdgcn_readlane(k_lo, l),
+                   __builtin_amdgcn_readlane(k_len, l),
+                   __builtin_amdgcn_readlane(k_slot, l)};
+        if (here < 64) break;
     }
-    return n - 1;
+    return j;
 }
 
 // A job of a row tile: ROWS rows of one key head's list, and the run of keys
@@ -242,21 +259,22 @@ struct RowJob {
 template <int ROWS>
 __device__ __forceinline__ RowJob row_job(const FullSeqs& seqs, int32_t Hk, int32_t rep, bool causal, bool fold, int32_t split,
                                           int32_t job, int lane) {
-    const int s = __builtin_amdgcn_readfirstlane(seq_of_job(seqs, job, lane));
+    const JobSeq s = seq_of_job(seqs, job, lane);
     RowJob j;
-    j.q_lo = seqs.q_lo(s);
-    j.q_len = seqs.q_len(s);
-    j.k_lo = seqs.k_lo(s);
-    j.k_len = seqs.k_len(s);
+    j.q_lo = s.q_lo, j.q_len = s.q_len, j.k_lo = s.k_lo, j.k_len = s.k_len;
     j.runs = full_runs(j.k_len, split);
     const int32_t tiles = (int32_t)(((int64_t)j.q_len * rep + ROWS - 1) / ROWS);
     // key heads first: with 8 of them (or a divisor) workgroups of one XCD,
     // which come round robin, share a head's keys in its L2
-    int32_t rest = job - seqs.job0(s);
+    int32_t rest = job - s.job0;
     j.kv_head = rest % Hk;
     rest /= Hk;
-    j.run = rest % j.runs;
-    j.tile = full_tile(rest / j.runs, tiles, causal, false, fold);
+    j.run = 0;
+    if (j.runs > 1) {
+        j.run = rest % j.runs;
+        rest /= j.runs;
+    }
+    j.tile = full_tile(rest, tiles, causal, false, fold);
     return j;
 }
 

@@ -312,14 +312,14 @@ __global__ __launch_bounds__(256) void full_join_kernel(const JoinArgs b) {
     const FwdArgs& a = b.f;
     __shared__ f32x4 part[256];
     __shared__ float sm[256], sl[256];
-    const int s = __builtin_amdgcn_readfirstlane(seq_of_job(a.s, blockIdx.x, threadIdx.x & 63));
-    const int32_t q_lo = a.s.q_lo(s), nrows = a.s.q_len(s) * a.rep, runs = full_runs(a.s.k_len(s), a.split);
-    const int32_t tiles = (nrows - 1) / b.rows + 1, kv_head = (blockIdx.x - a.s.job0(s)) % a.Hk, place = (blockIdx.x - a.s.job0(s)) / a.Hk;
+    const JobSeq s = seq_of_job(a.s, blockIdx.x, threadIdx.x & 63);
+    const int32_t q_lo = s.q_lo, nrows = s.q_len * a.rep, runs = full_runs(s.k_len, a.split);
+    const int32_t tiles = (nrows - 1) / b.rows + 1, kv_head = (blockIdx.x - s.job0) % a.Hk, place = (blockIdx.x - s.job0) / a.Hk;
     const int32_t tile = full_tile(place, tiles, a.causal, false, a.fold);
     const int groups = a.dv / 4, at_once = 256 / groups / b.lanes;
     const int g = threadIdx.x % groups, t = threadIdx.x / groups % b.lanes;
     // run 0; run r is r * Hk jobs on
-    const int64_t job = (int64_t)a.first_job + b.part0[s] + (int64_t)place * runs * a.Hk + kv_head, step = (int64_t)a.Hk * b.rows;
+    const int64_t job = (int64_t)a.first_job + b.part0[s.index] + (int64_t)place * runs * a.Hk + kv_head, step = (int64_t)a.Hk * b.rows;
     const int32_t left = min(b.rows, nrows - tile * b.rows);
     for (int32_t r0 = blockIdx.y * at_once; r0 < left; r0 += gridDim.y * at_once) {
         const int32_t rr = r0 + threadIdx.x / groups / b.lanes, row = tile * b.rows + rr;
