@@ -333,8 +333,10 @@ kmip_status_t kmip_fwd_noalloc(const void* Q, const void* K, const void* V, int6
  *  - causal != 0: the queries are the last of the sequence's positions: query t
  *    of a sequence with m queries and n keys sees keys 0 .. t + n - m.
  *  - A query that sees no key has out = 0 and lse = -inf.
- *  - NaN and Inf in the inputs give undefined (but memory-safe) results in the
- *    rows of their own sequence.
+ *  - NaN and Inf in the inputs, also at keys that the mask hides, and scores beyond 2^24
+ *    (|scale q.k|: float32 resolves them to 1 at best) give undefined (but
+ *    memory-safe) results in the rows of their own sequence.
+ *  - Outputs overlap neither inputs nor each other.
  *  - Nq * H and Nk below 2^31 - 4096; products of sizes and strides may pass 32 bits.
  *  - workspace: kmip_full_fwd_workspace_size() bytes, 256-byte aligned; the size
  *    depends on the offsets and lengths.  0 (then NULL is taken) where no sequence

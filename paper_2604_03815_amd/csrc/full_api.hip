@@ -54,7 +54,8 @@ bool width_ok(int32_t d) { return d == 16 || d == 32 || d == 64 || d == 128; }
 kmip_status_t check_call(const int32_t* q_offsets, const int32_t* k_offsets, const int32_t* k_lengths, int32_t G,
                          int64_t Nq, int64_t Nk, int32_t H, int32_t Hk, int32_t d, int32_t dv, Sequences* s) {
     constexpr int64_t kMost = (int64_t(1) << 31) - 4096;
-    if (Nq < 0 || Nk < 0 || Nk >= kMost) return record_error(KMIP_ERR_INVALID_ARG, "Nq=%lld, Nk=%lld out of range", (long long)Nq, (long long)Nk);
+    if (Nq < 0 || Nk < 0 || Nk >= kMost)
+        return record_error(KMIP_ERR_INVALID_ARG, "Nq=%lld, Nk=%lld out of range", (long long)Nq, (long long)Nk);
     if (H < 1 || Hk < 1 || H % Hk != 0)
         return record_error(KMIP_ERR_INVALID_ARG, "H=%d must be a multiple of the %d key heads", H, Hk);
     if (!width_ok(d) || !width_ok(dv))
@@ -71,9 +72,11 @@ kmip_status_t check_call(const int32_t* q_offsets, const int32_t* k_offsets, con
     }
     if (k_lengths != nullptr)
         for (int32_t g = 0; g < s->count; ++g) {
-            const int64_t slot = q_offsets == nullptr ? Nk : k_offsets != nullptr ? k_offsets[g + 1] - k_offsets[g] : q_offsets[g + 1] - q_offsets[g];
+            const int32_t* ko = k_offsets != nullptr ? k_offsets : q_offsets;
+            const int64_t slot = ko == nullptr ? Nk : ko[g + 1] - ko[g];
             if (k_lengths[g] < 0 || k_lengths[g] > slot)
-                return record_error(KMIP_ERR_INVALID_ARG, "k_lengths[%d]=%d outside [0, %lld]", g, k_lengths[g], (long long)slot);
+                return record_error(KMIP_ERR_INVALID_ARG, "k_lengths[%d]=%d outside [0, %lld]", g, k_lengths[g],
+                                    (long long)slot);
         }
     return KMIP_OK;
 }
@@ -88,7 +91,8 @@ bool finite_bits(float x) {   // (the sources are built without NaN tests)
 // streamed_of(seq) streamed rows each, into launches, the costliest sequences
 // first (ties in their order), so that the last jobs are short ones.
 template <typename Tiles, typename Kept, typename Streamed>
-kmip_status_t cut(std::vector<Seq>& seqs, bool causal, const Tiles& tiles_of, const Kept& kept_of, const Streamed& streamed_of, FullPlan* p) {
+kmip_status_t cut(std::vector<Seq>& seqs, bool causal, const Tiles& tiles_of, const Kept& kept_of,
+                  const Streamed& streamed_of, FullPlan* p) {
     auto cost = [](const Seq& s) { return (int64_t)std::max(s.q_len, 1) * std::max(s.k_len, 1); };
     std::stable_sort(seqs.begin(), seqs.end(), [&](const Seq& x, const Seq& y) { return cost(x) > cost(y); });
     p->jobs = 0;
@@ -122,7 +126,8 @@ kmip_status_t cut(std::vector<Seq>& seqs, bool causal, const Tiles& tiles_of, co
                 l.tile_rows = (int32_t)std::max<int64_t>(l.tile_rows, std::min<int64_t>(p->rows, kept_of(s)));
             }
             jobs += tiles * runs;
-            if (p->jobs + jobs >= (int64_t(1) << 31) - 1) return record_error(KMIP_ERR_INVALID_ARG, "too many rows and key runs for one call");
+            if (p->jobs + jobs >= (int64_t(1) << 31) - 1)
+                return record_error(KMIP_ERR_INVALID_ARG, "too many rows and key runs for one call");
         }
         l.jobs = (int32_t)jobs;
         l.tile_jobs = (int32_t)tile_jobs;
@@ -162,8 +167,8 @@ int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 //   d = 128, 8 heads, causal, forward: 8192 tokens 182, 165; 4096 tokens 88, 71; 12 heads, 3000 tokens, all
 //     pairs 87, 104 (288 tiles: two rounds on 256 CUs)
 template <typename Kept, typename Streamed>
-kmip_status_t plan(std::vector<Seq>& seqs, int32_t Hk, bool causal, const Kept& kept_of, const Streamed& streamed_of, int32_t width, bool only_halves,
-                   FullPlan* p) {
+kmip_status_t plan(std::vector<Seq>& seqs, int32_t Hk, bool causal, const Kept& kept_of, const Streamed& streamed_of,
+                   int32_t width, bool only_halves, FullPlan* p) {
     auto tiles = [&](const Seq& s, int64_t rows) { return (kept_of(s) + rows - 1) / rows * Hk; };
     int64_t kept = 0, jobs = 0, work = 0, work32 = 0, longest = 0;
     for (const Seq& s : seqs) {
@@ -180,7 +185,8 @@ kmip_status_t plan(std::vector<Seq>& seqs, int32_t Hk, bool causal, const Kept& 
     const bool rounds = jobs >= half_slots && (causal || 4 * jobs >= 3 * round_up(jobs, half_slots));
     const int64_t least = width <= 64 || jobs <= half_slots ? 1024 : 2048;
     const bool halves = width <= 192 ? jobs <= 2 * kSlots && work >= jobs * least
-                                     : (jobs <= 2 * kSlots && work >= jobs * 6144) || (rounds && jobs < kSlots && work >= jobs * 2048);
+                                     : (jobs <= 2 * kSlots && work >= jobs * 6144) ||
+                                           (rounds && jobs < kSlots && work >= jobs * 2048);
     p->halves = p->rows == 128 && (only_halves || halves) ? 2 : 1;
     int64_t run = 0;
     if (p->rows == 32)
@@ -197,7 +203,9 @@ kmip_status_t plan_rows(const Sequences& sq, int32_t H, int32_t Hk, bool causal,
     std::vector<Seq> seqs;
     for (int32_t g = 0; g < sq.count; ++g)
         if (sq.at(g).q_len > 0) seqs.push_back(sq.at(g));
-    return plan(seqs, Hk, causal, [=](const Seq& s) { return s.q_len * rep; }, [](const Seq& s) { return (int64_t)s.k_len; }, width, false, p);
+    return plan(
+        seqs, Hk, causal, [=](const Seq& s) { return s.q_len * rep; }, [](const Seq& s) { return (int64_t)s.k_len; }, width,
+        false, p);
 }
 
 // Key tiles cover every slot, since rows without a gradient are written too.
@@ -206,7 +214,9 @@ kmip_status_t plan_keys(const Sequences& sq, int32_t H, int32_t Hk, bool causal,
     std::vector<Seq> seqs;
     for (int32_t g = 0; g < sq.count; ++g)
         if (sq.at(g).k_slot > 0) seqs.push_back(sq.at(g));
-    return plan(seqs, Hk, causal, [](const Seq& s) { return (int64_t)s.k_slot; }, [=](const Seq& s) { return s.q_len * rep; }, width, width == 256, p);
+    return plan(
+        seqs, Hk, causal, [](const Seq& s) { return (int64_t)s.k_slot; }, [=](const Seq& s) { return s.q_len * rep; }, width,
+        width == 256, p);
 }
 
 // (The workspace queries plan without a mask: a causal plan never has more runs, since a mask only makes two groups, and so
@@ -243,10 +253,13 @@ BwdLayout bwd_layout(const FullPlan& dq, const FullPlan& dkv, int64_t Nq, int32_
 // A stride in values between rows of a 16-bit tensor that the kernels read 16
 // bytes at a time.
 kmip_status_t check_strides(const char* name, const void* p, int64_t row, int64_t head) {
-    if ((reinterpret_cast<uintptr_t>(p) & 15u) != 0) return record_error(KMIP_ERR_INVALID_ARG, "%s must be 16-byte aligned", name);
+    if ((reinterpret_cast<uintptr_t>(p) & 15u) != 0)
+        return record_error(KMIP_ERR_INVALID_ARG, "%s must be 16-byte aligned", name);
     if (row < 0 || head < 0 || row % 8 != 0 || head % 8 != 0)
-        return record_error(KMIP_ERR_INVALID_ARG, "%s: strides %lld, %lld must be multiples of 8 values", name, (long long)row, (long long)head);
-    if (row >= (int64_t(1) << 23)) return record_error(KMIP_ERR_UNSUPPORTED, "%s: %lld values between rows", name, (long long)row);
+        return record_error(KMIP_ERR_INVALID_ARG, "%s: strides %lld, %lld must be multiples of 8 values", name, (long long)row,
+                            (long long)head);
+    if (row >= (int64_t(1) << 23))
+        return record_error(KMIP_ERR_UNSUPPORTED, "%s: %lld values between rows", name, (long long)row);
     return KMIP_OK;
 }
 
@@ -272,8 +285,10 @@ kmip_status_t fill_call(const void* Q, const void* K, const void* V, int32_t dty
 
 kmip_status_t check_workspace(const void* ws, size_t bytes, size_t need) {
     if (need == 0) return KMIP_OK;
-    if (ws == nullptr || bytes < need) return record_error(KMIP_ERR_WORKSPACE, "workspace of %zu bytes < %zu required", bytes, need);
-    if ((reinterpret_cast<uintptr_t>(ws) & (kAlign - 1)) != 0) return record_error(KMIP_ERR_WORKSPACE, "workspace must be 256-byte aligned");
+    if (ws == nullptr || bytes < need)
+        return record_error(KMIP_ERR_WORKSPACE, "workspace of %zu bytes < %zu required", bytes, need);
+    if ((reinterpret_cast<uintptr_t>(ws) & (kAlign - 1)) != 0)
+        return record_error(KMIP_ERR_WORKSPACE, "workspace must be 256-byte aligned");
     return KMIP_OK;
 }
 

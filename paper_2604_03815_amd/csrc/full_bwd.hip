@@ -285,7 +285,8 @@ __global__ __launch_bounds__(256 * HALVES, KEYS == 128 ? 2 : 1) void full_dkv_ke
             }
             // rows of the block that do not see the key, or lie behind the last token
             if (tok + 32 * b < t_all || tok + 32 * b + 32 > q_len) {
-                const int32_t from = a.causal ? key - off - tok - 32 * b - 4 * (lane >> 5) : 0, upto = q_len - tok - 32 * b - 4 * (lane >> 5);
+                const int32_t at0 = tok + 32 * b + 4 * (lane >> 5);
+                const int32_t from = a.causal ? key - off - at0 : 0, upto = q_len - at0;
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     const int i = (r & 3) + 8 * (r >> 2);
@@ -304,8 +305,9 @@ __global__ __launch_bounds__(256 * HALVES, KEYS == 128 ? 2 : 1) void full_dkv_ke
                 const s16x8 p = round8<T>(s, i), x = round8<T>(dp, i);   // rounded, the operands of the products
 #pragma unroll
                 for (int t = 0; t < (kTK > kTV ? kTK : kTV); ++t) {
-                    if (t < kTV) dv[t < kTV ? t : 0] = T::mfma(in.y_columns(t < kTV ? t : 0, at + (32 * b + 16 * i) * 2 * DV), p, dv[t < kTV ? t : 0]);
-                    if (t < kTK) dk[t < kTK ? t : 0] = T::mfma(in.x_columns(t < kTK ? t : 0, at + (32 * b + 16 * i) * 2 * DK), x, dk[t < kTK ? t : 0]);
+                    const int tv = t < kTV ? t : 0, tk = t < kTK ? t : 0;
+                    if (t < kTV) dv[tv] = T::mfma(in.y_columns(tv, at + (32 * b + 16 * i) * 2 * DV), p, dv[tv]);
+                    if (t < kTK) dk[tk] = T::mfma(in.x_columns(tk, at + (32 * b + 16 * i) * 2 * DK), x, dk[tk]);
                 }
             }
         }
@@ -319,7 +321,8 @@ __global__ __launch_bounds__(256 * HALVES, KEYS == 128 ? 2 : 1) void full_dkv_ke
     if constexpr (KEYS == 128) {
         const int32_t most = (n + HALVES - 1) / HALVES, mine = half == 0 ? most : n - most, begin = first + half * most;
         const int32_t tok0 = mine > 0 ? t_lo + begin % per * kTile : 0;
-        int32_t hr = mine > 0 ? begin / per : 0, tok = tok0, now = tok0;   // of the tile that is fetched next, of the one in use
+        // of the tile that is fetched next, of the one in use
+        int32_t hr = mine > 0 ? begin / per : 0, tok = tok0, now = tok0;
         auto next = [&](int32_t t) { return t + kTile < q_len ? t + kTile : t_lo; };
         stream_tiles(
             most, mine,
@@ -413,7 +416,8 @@ __global__ __launch_bounds__(256) void full_sum_kernel(const SumArgs a) {
     const int i = blockIdx.y * 256 + threadIdx.x, rr = i / groups, g = i % groups;
     const int32_t row = tile * a.rows + rr;
     if (rr >= a.rows || row >= nrows) return;
-    const float* p = a.part[which] + (((int64_t)a.first_job + a.part0[s.index] + (int64_t)place * runs * a.Hk + kv_head) * a.rows + rr) * width + 4 * g;
+    const int64_t job = (int64_t)a.first_job + a.part0[s.index] + (int64_t)place * runs * a.Hk + kv_head;
+    const float* p = a.part[which] + (job * a.rows + rr) * width + 4 * g;
     const int64_t step = (int64_t)a.Hk * a.rows * width;
     f32x4 x = *reinterpret_cast<const f32x4*>(p);
 #pragma unroll 4
@@ -430,12 +434,14 @@ hipError_t launch_sum(SumArgs& b, const BwdArgs& a, const FullLaunch& l, const F
     b.first_job = l.first_job, b.rows = p.rows, b.split = p.split, b.Hk = a.Hk, b.rep = a.rep;
     b.causal = a.causal, b.fold = l.fold, b.keys = keys;
     const int32_t widest = b.width[0] > b.width[1] ? b.width[0] : b.width[1];
-    hipLaunchKernelGGL((full_sum_kernel<T>), dim3(l.tile_jobs, (p.rows * (widest / 4) + 255) / 256, keys ? 2 : 1), dim3(256), 0, stream, b);
+    const dim3 grid(l.tile_jobs, (p.rows * (widest / 4) + 255) / 256, keys ? 2 : 1);
+    hipLaunchKernelGGL((full_sum_kernel<T>), grid, dim3(256), 0, stream, b);
     return hipGetLastError();
 }
 
 template <typename T, int DK, int DV>
-hipError_t launch_bwd(const FullCall& f, const FullPlan& dq, const FullPlan& dkv, const FullBwdSpace& ws, hipStream_t stream) {
+hipError_t launch_bwd(const FullCall& f, const FullPlan& dq, const FullPlan& dkv, const FullBwdSpace& ws,
+                      hipStream_t stream) {
     BwdArgs a{};
     a.q = reinterpret_cast<const char*>(f.q);
     a.k = reinterpret_cast<const char*>(f.k);
@@ -492,9 +498,11 @@ hipError_t launch_bwd(const FullCall& f, const FullPlan& dq, const FullPlan& dkv
 
 }  // namespace
 
-hipError_t launch_full_bwd(const FullCall& f, const FullPlan& dq, const FullPlan& dkv, const FullBwdSpace& ws, hipStream_t stream) {
+hipError_t launch_full_bwd(const FullCall& f, const FullPlan& dq, const FullPlan& dkv, const FullBwdSpace& ws,
+                           hipStream_t stream) {
 #define KMIP_FULL_CASE(DK, DV) \
-    if (f.d == DK && f.dv == DV) return f.fp16 ? launch_bwd<Fp16, DK, DV>(f, dq, dkv, ws, stream) : launch_bwd<Bf16, DK, DV>(f, dq, dkv, ws, stream);
+    if (f.d == DK && f.dv == DV) \
+        return f.fp16 ? launch_bwd<Fp16, DK, DV>(f, dq, dkv, ws, stream) : launch_bwd<Bf16, DK, DV>(f, dq, dkv, ws, stream);
 #define KMIP_FULL_BWD(DK) KMIP_FULL_CASE(DK, 16) KMIP_FULL_CASE(DK, 32) KMIP_FULL_CASE(DK, 64) KMIP_FULL_CASE(DK, 128)
     KMIP_FULL_BWD(16)
     KMIP_FULL_BWD(32)

@@ -43,8 +43,8 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
-// The two types.  kUp: the forward's weights are 2^kUp times as large (below
-// 2^15 in float16, whose values below 2^-14 lose bits).
+// The two types.  kUp: the forward's weights are 2^kUp times as large (2^14 at
+// most in float16, twice that where scores reach 2^24 and the reference is rounded; its values below 2^-14 lose bits).
 struct Bf16 {
     static constexpr float kUp = 0.0f;
     static __device__ __forceinline__ f32x16 mfma(s16x8 a, s16x8 b, f32x16 c) {
@@ -56,7 +56,7 @@ struct Bf16 {
 };
 
 struct Fp16 {
-    static constexpr float kUp = 7.0f;
+    static constexpr float kUp = 6.0f;
     static __device__ __forceinline__ f32x16 mfma(s16x8 a, s16x8 b, f32x16 c) {
         return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0,
                                                       0);
@@ -109,7 +109,9 @@ struct Operands {
             }
         }
     }
-    __device__ __forceinline__ s16x8 rows(int t, uint32_t at) const { return *(const KMIP_LDS s16x8*)(uintptr_t)(row[t] + at); }
+    __device__ __forceinline__ s16x8 rows(int t, uint32_t at) const {
+        return *(const KMIP_LDS s16x8*)(uintptr_t)(row[t] + at);
+    }
     __device__ __forceinline__ s16x8 columns(int t, uint32_t at) const {
         const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((KMIP_LDS s16x4*)(uintptr_t)(tr[0][t] + at));
         const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((KMIP_LDS s16x4*)(uintptr_t)(tr[1][t] + at));
@@ -131,7 +133,9 @@ __device__ __forceinline__ float2 both_halves(float x) {
 
 // x, uniform over the wave, in scalar registers.
 __device__ __forceinline__ uint32_t uniform(uint32_t x) { return __builtin_amdgcn_readfirstlane(x); }
-__device__ __forceinline__ uint64_t uniform(uint64_t x) { return (uint64_t)uniform((uint32_t)(x >> 32)) << 32 | uniform((uint32_t)x); }
+__device__ __forceinline__ uint64_t uniform(uint64_t x) {
+    return (uint64_t)uniform((uint32_t)(x >> 32)) << 32 | uniform((uint32_t)x);
+}
 
 // Memory to LDS, 16 bytes a lane: lane l's 16 bytes at base + off go to
 // lds + 16 l (base and lds uniform; the LDS address travels in m0, which is left
@@ -233,7 +237,8 @@ __device__ __forceinline__ JobSeq seq_of_job(const FullSeqs& s, int32_t job, int
     int n = 0;
     for (int i = 0; i < s.count; i += 64) {
         const int e = i + lane < s.count ? i + lane : s.count - 1;
-        const int32_t q_lo = s.q_lo(e), q_len = s.q_len(e), job0 = s.job0(e), k_lo = s.k_lo(e), k_len = s.k_len(e), k_slot = s.k_slot(e);
+        const int32_t q_lo = s.q_lo(e), q_len = s.q_len(e), job0 = s.job0(e);
+        const int32_t k_lo = s.k_lo(e), k_len = s.k_len(e), k_slot = s.k_slot(e);
         const int here = __popcll(__ballot(i + lane < s.count && job0 <= job));
         if (here == 0) break;
         n = i + here;
@@ -257,8 +262,8 @@ struct RowJob {
 };
 
 template <int ROWS>
-__device__ __forceinline__ RowJob row_job(const FullSeqs& seqs, int32_t Hk, int32_t rep, bool causal, bool fold, int32_t split,
-                                          int32_t job, int lane) {
+__device__ __forceinline__ RowJob row_job(const FullSeqs& seqs, int32_t Hk, int32_t rep, bool causal, bool fold,
+                                          int32_t split, int32_t job, int lane) {
     const JobSeq s = seq_of_job(seqs, job, lane);
     RowJob j;
     j.q_lo = s.q_lo, j.q_len = s.q_len, j.k_lo = s.k_lo, j.k_len = s.k_len;
@@ -338,7 +343,8 @@ __device__ __forceinline__ s16x4 round4(const f32x4& x, float f) {
 // the streamed rows lie in LDS: buffers of kTile rows of both tensors.
 template <int DK, int DV, int TILE>
 struct Buffers {
-    static constexpr int kTile = TILE, kFirst = TILE * 2 * DK, kBytes = kFirst + TILE * 2 * DV;   // the first tensor's, both tensors' bytes
+    // the first tensor's, both tensors' bytes
+    static constexpr int kTile = TILE, kFirst = TILE * 2 * DK, kBytes = kFirst + TILE * 2 * DV;
     // waves that load a tensor: all four, or two where its tile has only two loads
     static constexpr int kPartsK = kFirst >= 4096 ? 4 : 2, kPartsV = TILE * 2 * DV >= 4096 ? 4 : 2;
     // the same for a wave with buffers of its own: its loads

@@ -95,7 +95,7 @@ struct FwdWave {
         const float2 tops = both_halves(top);
         top = fmaxf(tops.x, tops.y);
         // The reference follows the maximum only where a weight would pass 2^8: bfloat16
-        // weights keep their relative precision at any reference; float16 ones are 2^7
+        // weights keep their relative precision at any reference; float16 ones are 2^6
         // times as large (T::kUp), so that small ones have their bits too.
         if (__any((top - m) * c > 8.0f)) {
             const float to = fmaxf(top, m);
@@ -217,7 +217,8 @@ __global__ __launch_bounds__(256 * HALVES, ROWS == 128 ? 2 : 1) void full_fwd_ke
         wait_and_sync();
         if (half == 1) return;
         const float mo = sm[wave][lane], top = fmaxf(mc, mo);
-        const float f = mc == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mc - top), g = mo == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mo - top);
+        const float f = mc == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mc - top);
+        const float g = mo == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mo - top);
         l = l * f + sl[wave][lane] * g;
         mc = top;
 #pragma unroll
@@ -314,12 +315,14 @@ __global__ __launch_bounds__(256) void full_join_kernel(const JoinArgs b) {
     __shared__ float sm[256], sl[256];
     const JobSeq s = seq_of_job(a.s, blockIdx.x, threadIdx.x & 63);
     const int32_t q_lo = s.q_lo, nrows = s.q_len * a.rep, runs = full_runs(s.k_len, a.split);
-    const int32_t tiles = (nrows - 1) / b.rows + 1, kv_head = (blockIdx.x - s.job0) % a.Hk, place = (blockIdx.x - s.job0) / a.Hk;
+    const int32_t tiles = (nrows - 1) / b.rows + 1;
+    const int32_t kv_head = (blockIdx.x - s.job0) % a.Hk, place = (blockIdx.x - s.job0) / a.Hk;
     const int32_t tile = full_tile(place, tiles, a.causal, false, a.fold);
     const int groups = a.dv / 4, at_once = 256 / groups / b.lanes;
     const int g = threadIdx.x % groups, t = threadIdx.x / groups % b.lanes;
     // run 0; run r is r * Hk jobs on
-    const int64_t job = (int64_t)a.first_job + b.part0[s.index] + (int64_t)place * runs * a.Hk + kv_head, step = (int64_t)a.Hk * b.rows;
+    const int64_t job = (int64_t)a.first_job + b.part0[s.index] + (int64_t)place * runs * a.Hk + kv_head;
+    const int64_t step = (int64_t)a.Hk * b.rows;
     const int32_t left = min(b.rows, nrows - tile * b.rows);
     for (int32_t r0 = blockIdx.y * at_once; r0 < left; r0 += gridDim.y * at_once) {
         const int32_t rr = r0 + threadIdx.x / groups / b.lanes, row = tile * b.rows + rr;
@@ -329,7 +332,8 @@ __global__ __launch_bounds__(256) void full_join_kernel(const JoinArgs b) {
         float top = -INFINITY, sum = 0.0f;
         f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
         auto add = [&](float m, float l, const f32x4& y) {   // m: -inf for a run without a key that the row sees
-            const float to = fmaxf(fmaxf(top, m), -1e30f), f = __builtin_amdgcn_exp2f(top - to), h = __builtin_amdgcn_exp2f(m - to);
+            const float to = fmaxf(fmaxf(top, m), -1e30f);
+            const float f = __builtin_amdgcn_exp2f(top - to), h = __builtin_amdgcn_exp2f(m - to);
             top = fmaxf(top, m);
             sum = sum * f + l * h;
             x = x * f + y * h;
@@ -423,7 +427,8 @@ hipError_t launch_fwd(const FullCall& f, const FullPlan& p, float* part_o, float
 
 hipError_t launch_full_fwd(const FullCall& f, const FullPlan& p, float* part_o, float* part_ml, hipStream_t stream) {
 #define KMIP_FULL_CASE(DK, DV) \
-    if (f.d == DK && f.dv == DV) return f.fp16 ? launch_fwd<Fp16, DK, DV>(f, p, part_o, part_ml, stream) : launch_fwd<Bf16, DK, DV>(f, p, part_o, part_ml, stream);
+    if (f.d == DK && f.dv == DV) \
+        return f.fp16 ? launch_fwd<Fp16, DK, DV>(f, p, part_o, part_ml, stream) : launch_fwd<Bf16, DK, DV>(f, p, part_o, part_ml, stream);
 #define KMIP_FULL_FWD(DK) KMIP_FULL_CASE(DK, 16) KMIP_FULL_CASE(DK, 32) KMIP_FULL_CASE(DK, 64) KMIP_FULL_CASE(DK, 128)
     KMIP_FULL_FWD(16)
     KMIP_FULL_FWD(32)

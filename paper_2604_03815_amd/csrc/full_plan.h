@@ -85,7 +85,8 @@ struct FullBwdSpace {
     float *dq, *dk, *dv;           // [job][rows][width] sums of runs
 };
 // dQ first (plan dq; it also writes lse2 and D), then dK and dV (plan dkv).
-hipError_t launch_full_bwd(const FullCall& f, const FullPlan& dq, const FullPlan& dkv, const FullBwdSpace& ws, hipStream_t stream);
+hipError_t launch_full_bwd(const FullCall& f, const FullPlan& dq, const FullPlan& dkv, const FullBwdSpace& ws,
+                           hipStream_t stream);
 hipError_t launch_full_fwd(const FullCall& f, const FullPlan& p, float* part_o, float* part_ml, hipStream_t stream);
 
 }  // namespace kmip

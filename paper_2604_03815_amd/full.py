@@ -14,6 +14,8 @@ how many keys at the start of each slot are in use (None: all), for caches
 with room.  Without graph_offsets there is one sequence.  ``causal``: the queries are the
 last positions of their sequence, query t of m sees keys 0 .. t + n - m of n.
 The offsets and lengths are read when the call is made: a captured call keeps them.
+Inputs are finite (rows behind the keys in use may hold anything: they are not read);
+given outputs overlap neither inputs nor each other.
 """
 from __future__ import annotations
 
@@ -178,8 +180,8 @@ def full_fwd(q, k_, v, scale: float, graph_offsets: Optional[Sequence[int]] = No
         out = _new(q, (Nq, H, dv), q.dtype)
     if lse is None:
         lse = q.new_empty((Nq, H), dtype=torch.float32)
-    _launch(dev, lib.kmip_full_fwd, q.data_ptr(), k_.data_ptr(), v.data_ptr(), code, None if whole else _strides(q, k_, v), *ptrs, G, *sizes, float(scale),
-            1 if causal else 0, out.data_ptr(), lse.data_ptr(), _address(buf), 0 if buf is None else buf.numel())
+    _launch(dev, lib.kmip_full_fwd, q.data_ptr(), k_.data_ptr(), v.data_ptr(), code, None if whole else _strides(q, k_, v), *ptrs, G,
+            *sizes, float(scale), 1 if causal else 0, out.data_ptr(), lse.data_ptr(), _address(buf), 0 if buf is None else buf.numel())
     return out, lse
 
 

@@ -93,6 +93,24 @@ def test_small_float16_weights(m):
     assert (lse.double() - torch.logsumexp(s, 0)).abs().max() <= 2.0 ** -18
 
 
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("m,n", [(1, 700), (1, 5000), (600, 600)])
+def test_large_scores(m, n, dtype):
+    """Scores of nearly 2^24, all alike, of either sign: every key has the same weight."""
+    d = 16
+    for sign in (1.0, -1.0):
+        q = torch.full((m, 1, d), 1000.0 * sign, dtype=dtype, device="cuda")
+        k = torch.full((n, 1, d), 1000.0, dtype=dtype, device="cuda")
+        v = normal(1, n, 1, d, dtype=dtype)
+        out, lse = kmip.full_fwd(q, k, v, 1.0)
+        want = v.double().mean(0)
+        # weights and the result, half a step each, and n additions in 32 bits each of the sum and its normaliser
+        u = torch.finfo(dtype).eps / 2
+        assert ((out.double() - want).abs() <= (u + 2 * n * 2.0 ** -24) * v.double().abs().mean(0) + u * want.abs()).all()
+        score = d * 1000.0 * 1000.0 * sign
+        assert (lse.double() - score - math.log(n)).abs().max() <= 2.0 ** -22 * abs(score)
+
+
 @pytest.mark.parametrize("heads,kv,d,dv,causal", [(8, 2, 64, 64, True), (3, 3, 16, 32, False), (4, 1, 128, 128, True)])
 def test_cache_with_room(heads, kv, d, dv, causal):
     """Rows behind a slot's keys in use are not read (NaN there) and get gradient 0; nothing beside the outputs is written."""
