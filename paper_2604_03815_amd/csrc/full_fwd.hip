@@ -25,14 +25,14 @@
 //
 // Measured (MI355X) and what bounds it:
 //   - d = 128: matrix and vector instructions, which overlap in part, and power
-//     (2.0 to 2.2 GHz).  A prompt of 16,384 tokens, 8 heads on 2 key heads, causal: 538
-//     us, 1.02 PFLOP/s (a library product of 8192^3: 1.2); the matrix units are busy 48% of the
+//     (2.0 to 2.2 GHz).  A prompt of 16,384 tokens, 8 heads on 2 key heads, causal: 545
+//     us, 1.01 PFLOP/s (a library product of 8192^3: 1.2); the matrix units are busy 48% of the
 //     time, the vector units issue 40% of it.  Interleaving the scores of a
 //     tile, the weights of the one before and the product of the one before that
 //     in one block of code gave nothing (580 us for 584 then).
 //   - d <= 64: vector issue.  64 keys of 32 rows at d = 64 are 98 vector
 //     instructions, 32 exponentials and 16 products: 1014 clocks if nothing
-//     waits, 1219 measured (17 prompts of up to 4000 tokens, 16 heads on 4, 215 us).
+//     waits, 1219 measured (17 prompts of up to 4000 tokens, 16 heads on 4, 220 us).
 //   - few rows: the cache's bytes.  One token over each of 64 caches of up to 32,767,
 //     32 heads on 8, d = 128: 203 us, 5.5 TB/s (a large copy moves 4.9, reads alone
 //     5.3 to 6.5), and 6 us for the join.
