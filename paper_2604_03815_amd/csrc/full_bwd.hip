@@ -92,7 +92,7 @@ __global__ __launch_bounds__(256 * HALVES, ROWS == 128 ? 2 : 1) void full_dq_ker
     const int32_t lim = sees(row), lim_first = sees(row0), lim_last = row0 < nrows ? sees(row0 + 31) : 0;
     const int32_t lo = a.split > 0 ? j.run * a.split : 0;
     int32_t hi = sees(j.tile * ROWS + ROWS - 1);
-    if (j.runs > 1) hi = min(hi, lo + a.split);
+    if (j.runs > 1) hi = full_run_end(lo, hi, a.split);
 
     const char* kp = a.k + (int64_t)j.k_lo * a.k_row + j.kv_head * a.k_head;
     const char* vp = a.v + (int64_t)j.k_lo * a.v_row + j.kv_head * a.v_head;

@@ -162,7 +162,7 @@ __global__ __launch_bounds__(256 * HALVES, ROWS == 128 ? 2 : 1) void full_fwd_ke
 
     const int32_t lo = a.split > 0 ? j.run * a.split : 0;
     int32_t hi = sees(j.tile * ROWS + ROWS - 1);
-    if (a.split > 0) hi = min(hi, lo + a.split);
+    if (a.split > 0) hi = full_run_end(lo, hi, a.split);
     const int32_t lim_first = sees(row0), lim_last = row0 < nrows ? sees(row0 + 31) : 0;
     const float c = a.scale * kLog2e;
     const char* kp = a.k + (int64_t)j.k_lo * a.k_row + j.kv_head * a.k_head;

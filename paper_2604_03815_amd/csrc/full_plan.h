@@ -37,6 +37,11 @@ __host__ __device__ inline int32_t full_runs(int64_t streamed, int32_t split) {
     return split > 0 && streamed > split ? (int32_t)((streamed - 1) / split + 1) : 1;
 }
 
+// End of a tile's run from lo on, of streamed rows that end at hi (both below 2^31, while lo + split may pass it).
+__host__ __device__ inline int32_t full_run_end(int32_t lo, int32_t hi, int32_t split) {
+    return hi - lo > split ? lo + split : hi;
+}
+
 // Tile of place i of n.  Causal tiles differ in work; `falling`: tile 0 has the
 // most.  Most first while workgroups queue for the CUs.  Where all of them are
 // resident at once, the second half in the opposite order (fold), so that the
