@@ -78,6 +78,13 @@ def _check_devices(*named):
     return dev
 
 
+def _written(*given):
+    """The caller's own tensors among these were written: autograd, which the launch went past, counts it like an operation of torch's."""
+    given = [t for t in given if t is not None]
+    if given:
+        torch.autograd.graph.increment_version(given)
+
+
 def _launch(device, call, *args):
     """call(*args, stream) with the tensors' device current, on its current stream."""
     i = device.index
@@ -173,6 +180,7 @@ def full_fwd(q, k_, v, scale: float, graph_offsets: Optional[Sequence[int]] = No
     keep, ptrs, G = _sequences(graph_offsets, key_offsets, key_lengths)
     dev = _check_devices((q, "Q"), (k_, "K"), (v, "V"), (out, "out"), (lse, "lse"))
     lib = load()
+    given = out, lse
     buf = None
     if Nk >= FULL_LONG:
         buf = _scratch(workspace, lib.kmip_full_fwd_workspace_size(*ptrs, G, *sizes), dev)
@@ -182,6 +190,7 @@ def full_fwd(q, k_, v, scale: float, graph_offsets: Optional[Sequence[int]] = No
         lse = q.new_empty((Nq, H), dtype=torch.float32)
     _launch(dev, lib.kmip_full_fwd, q.data_ptr(), k_.data_ptr(), v.data_ptr(), code, None if whole else _strides(q, k_, v), *ptrs, G,
             *sizes, float(scale), 1 if causal else 0, out.data_ptr(), lse.data_ptr(), _address(buf), 0 if buf is None else buf.numel())
+    _written(*given)
     return out, lse
 
 
@@ -207,6 +216,7 @@ def full_bwd(q, k_, v, dout, out, lse, scale: float, graph_offsets: Optional[Seq
     dev = _check_devices((q, "Q"), (k_, "K"), (v, "V"), (dout, "dOut"), (out, "out"), (lse, "lse"), (dq, "dQ"), (dk, "dK"),
                          (dv, "dV"))
     lib = load()
+    given = dq, dk, dv
     buf = _scratch(workspace, lib.kmip_full_bwd_workspace_size(*ptrs, G, *sizes), dev)
     if dq is None:
         dq = _new(q, (Nq, H, d), q.dtype)
@@ -217,6 +227,7 @@ def full_bwd(q, k_, v, dout, out, lse, scale: float, graph_offsets: Optional[Seq
     _launch(dev, lib.kmip_full_bwd, q.data_ptr(), k_.data_ptr(), v.data_ptr(), dout.data_ptr(), out.data_ptr(), lse.data_ptr(),
             code, None if whole else _strides(q, k_, v, dout), *ptrs, G, *sizes, float(scale), 1 if causal else 0, dq.data_ptr(), dk.data_ptr(),
             dv.data_ptr(), _address(buf), 0 if buf is None else buf.numel())
+    _written(*given)
     return dq, dk, dv
 
 

@@ -15,7 +15,7 @@ import numpy as np
 import torch
 
 from ._lib import load
-from .full import _DTYPES, _address, _check_devices, _check_tensor, _launch as _launch_on, _new, _strides
+from .full import _DTYPES, _address, _check_devices, _check_tensor, _launch as _launch_on, _new, _strides, _written
 
 
 def rotary_frequencies(rot: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0,
@@ -114,6 +114,7 @@ def _launch(q, k_, positions, freqs, interleaved, magnitude, inverse, dtype, q_o
     if positions is not None:
         _check_positions(positions, N)
     dev = _check_devices((q, "q"), (k_, "k"), (q_out, "q_out"), (k_out, "k_out"), (positions, "positions"))
+    given = q_out, k_out
     if q_out is None:
         q_out = _new(q, (N, H, d), to)
     if k_ is not None and k_out is None:
@@ -124,6 +125,7 @@ def _launch(q, k_, positions, freqs, interleaved, magnitude, inverse, dtype, q_o
     _launch_on(dev, load().kmip_rotary, q.data_ptr(), q_out.data_ptr(), H, _address(k_), _address(k_out), H2, _DTYPES[q.dtype],
                _DTYPES[to], strides, _address(positions), f.__array_interface__["data"][0], N, d, 2 * len(f), 1 if interleaved else 0,
                float(magnitude), 1 if inverse else 0)
+    _written(*given)
     return q_out if k_ is None else (q_out, k_out)
 
 
