@@ -48,9 +48,18 @@ def _check_tensor(t, name, dtype, shape):
     return False
 
 
+def _check_written(t, name):
+    """A tensor to write into is no part of a graph of autograd's, which would go on with the gradient of its old values."""
+    if t.requires_grad and torch.is_grad_enabled():
+        raise ValueError(f"{name} requires a gradient: writing into it is not differentiable, call under torch.no_grad()")
+
+
 def _check_output(t, name, dtype, shape):
-    if t is not None and not _check_tensor(t, name, dtype, shape):
+    if t is None:
+        return
+    if not _check_tensor(t, name, dtype, shape):
         raise ValueError(f"{name} must be contiguous")
+    _check_written(t, name)
 
 
 def _new(like, shape, dtype):

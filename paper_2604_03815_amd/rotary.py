@@ -15,7 +15,7 @@ import numpy as np
 import torch
 
 from ._lib import load
-from .full import _DTYPES, _address, _check_devices, _check_tensor, _launch as _launch_on, _new, _strides, _written
+from .full import _DTYPES, _address, _check_devices, _check_tensor, _check_written, _launch as _launch_on, _new, _strides, _written
 
 
 def rotary_frequencies(rot: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0,
@@ -130,7 +130,11 @@ def _launch(q, k_, positions, freqs, interleaved, magnitude, inverse, dtype, q_o
 
 
 def _check_out(t, name, dtype, shape):
-    if t is None or _check_tensor(t, name, dtype, shape):
+    if t is None:
+        return True
+    whole = _check_tensor(t, name, dtype, shape)
+    _check_written(t, name)
+    if whole:
         return True
     N, heads, d = shape
     if t.numel():

@@ -52,3 +52,19 @@ def test_saved_tensor_turned_in_place(no_launch):
     kmip.rotary(q, freqs=F, q_out=q)
     with pytest.raises(RuntimeError, match="inplace"):
         y.sum().backward()
+
+
+def test_outputs_of_a_graph_are_refused(no_launch):
+    """A given output that requires a gradient would keep the gradient of the values it had."""
+    def of_graph(*shape, dtype=BF):
+        return torch.ones(*shape, dtype=dtype, requires_grad=True) * 2
+
+    calls = [lambda: kmip.full_fwd(*attend_args(), out=of_graph(40, 4, 16)), lambda: kmip.full_fwd(*attend_args(), lse=of_graph(40, 4, dtype=SF)),
+             lambda: kmip.full_bwd(*attend_args()[:3], z(40, 4, 16), z(40, 4, 16), z(40, 4, dtype=SF), 0.25, dk=of_graph(50, 2, 32)),
+             lambda: kmip.rotary(z(9, 2, 16), freqs=F, q_out=of_graph(9, 2, 16)),
+             lambda: kmip.rotary(z(9, 2, 16), z(9, 2, 16), freqs=F, k_out=of_graph(9, 4, 16)[:, ::2])]
+    for one in calls:
+        with pytest.raises(ValueError, match="requires a gradient"):
+            one()
+        with torch.no_grad():
+            one()
