@@ -13,6 +13,7 @@ from typing import Optional
 
 import numpy as np
 import torch
+from torch.autograd import forward_ad
 
 from ._lib import load
 from .full import _DTYPES, _address, _check_devices, _check_tensor, _check_written, _launch as _launch_on, _new, _strides, _written
@@ -75,13 +76,14 @@ def rotary(q, k_=None, positions=None, freqs=None, interleaved: bool = False, ma
     positions: int32 [N] on the device (None: row i is at position i); freqs: host float64 [rot / 2] (``rotary_frequencies``); dtype of the results
     (default: the inputs'): bfloat16, float16 or float32.  inverse turns back.  q_out, k_out: tensors to write into,
     q_out=q for in place.  Inputs and outputs may be views whose last dimension is contiguous (outputs must not overlap themselves).
-    Differentiable in q and k_ unless q_out or k_out is given.
+    Differentiable in q and k_ unless q_out or k_out is given; once, and in reverse mode only (dual tensors are refused).
     """
     if freqs is None:
         raise ValueError("freqs must be given (see rotary_frequencies)")
     given = q_out is not None or k_out is not None
     grad = torch.is_grad_enabled() and any(isinstance(t, torch.Tensor) and t.requires_grad for t in (q, k_))
-    if grad:
+    if grad or forward_ad._current_level >= 0 and _has_tangent(q, k_):
+        # (dual tensors go this way too: autograd refuses them, the launch would drop their tangents)
         if given:
             raise ValueError("q_out and k_out are not differentiable: leave them out, or call under torch.no_grad()")
         _rows(q, "q")
@@ -90,6 +92,10 @@ def rotary(q, k_=None, positions=None, freqs=None, interleaved: bool = False, ma
         got = _rotary_function().apply(q, k_, positions, freqs, interleaved, magnitude, inverse, dtype)
         return got[0] if k_ is None else got
     return _launch(q, k_, positions, freqs, interleaved, magnitude, inverse, dtype, q_out, k_out)
+
+
+def _has_tangent(*tensors):
+    return any(isinstance(t, torch.Tensor) and forward_ad.unpack_dual(t).tangent is not None for t in tensors)
 
 
 def _launch(q, k_, positions, freqs, interleaved, magnitude, inverse, dtype, q_out, k_out):

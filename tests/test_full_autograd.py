@@ -68,3 +68,19 @@ def test_outputs_of_a_graph_are_refused(no_launch):
             one()
         with torch.no_grad():
             one()
+
+
+def test_dual_tensors_are_refused(no_launch):
+    """No forward-mode derivative: an error, not a result without its tangent."""
+    forward_ad = torch.autograd.forward_ad
+    with forward_ad.dual_level():
+        x = forward_ad.make_dual(z(9, 2, 16), z(9, 2, 16))
+        for q, k in ((x, None), (z(9, 2, 16), x)):
+            with pytest.raises(NotImplementedError):
+                kmip.rotary(q, k, freqs=F)
+            with pytest.raises(ValueError, match="differentiable"):
+                kmip.rotary(q, k, freqs=F, q_out=z(9, 2, 16))
+        with pytest.raises(NotImplementedError):
+            kmip.full_attention(z(9, 2, 16), x, z(9, 2, 16), 0.25)
+        y = kmip.rotary(z(9, 2, 16), freqs=F)   # tensors without a tangent are as ever
+        assert forward_ad.unpack_dual(y).tangent is None
