@@ -27,7 +27,7 @@ def rotary_frequencies(rot: int, base: float = 10000.0, scaling: str = "none", f
       "linear"  every frequency divided by the factor;
       "base"    base times factor^(rot / (rot - 2)): the fastest pair as it was, the slowest divided by the factor;
       "blend"   pairs that turn less than ``slow_turns`` times in the original length divided by the factor, those that turn more
-                than ``fast_turns`` times as they were, a linear blend in between; magnitude 0.1 log(factor) + 1.
+                than ``fast_turns`` times as they were, a linear blend in between; magnitude 0.1 log(factor) + 1 (1 for a factor below 1).
     """
     if rot < 2 or rot % 2:
         raise ValueError("rot must be even and at least 2")
@@ -45,7 +45,7 @@ def rotary_frequencies(rot: int, base: float = 10000.0, scaling: str = "none", f
     if original_length is None or not 0 <= slow_turns < fast_turns:
         raise ValueError("blend needs original_length and 0 <= slow_turns < fast_turns")
     keep = np.clip((original_length * freqs / (2 * math.pi) - slow_turns) / (fast_turns - slow_turns), 0.0, 1.0)
-    return freqs * keep + freqs / factor * (1.0 - keep), 0.1 * math.log(factor) + 1.0
+    return freqs * keep + freqs / factor * (1.0 - keep), 0.1 * math.log(max(factor, 1.0)) + 1.0
 
 
 class Rotary:
