@@ -78,6 +78,8 @@ class KMIPAttention(torch.nn.Module):
     positions (int32 [N] on the device; None for one graph: 0, 1, ..) are those of the nodes.
     """
 
+    rotary: Optional[Rotary] = None   # (of layers that were pickled before there was one)
+
     def __init__(self, d_model: int, heads: int, d_k: int, d_v: Optional[int] = None, k: int = 16,
                  k_schedule: Optional[Callable[[int], int]] = None, attn_dropout: float = 0.0,
                  variant: int = 0, device=None, generator: Optional[torch.Generator] = None,
@@ -124,7 +126,9 @@ class KMIPAttention(torch.nn.Module):
         kk = self.current_k()
         if self.training:
             self.step += 1
-        q, k, v = self.project(x.float(), positions, graph_offsets)
+        # (a subclass may have project(x) alone, as long as nothing is to be turned)
+        where = () if self.rotary is None and positions is None else (positions, graph_offsets)
+        q, k, v = self.project(x.float(), *where)
         rate = self.attn_dropout if self.training else 0.0
         if rate > 0.0 and keep is None:
             keep = (torch.rand(q.shape[0], self.heads, kk, device=q.device) >= rate).to(torch.uint8)
