@@ -56,6 +56,10 @@ struct FwdArgs {
     FullSeqs s;
 };
 
+// The reference of a row that has seen no key: below every score, and finite, so that no
+// difference of two infinities is formed (these sources are built for code without NaN).
+constexpr float kNoKey = -3.402823466e38f;
+
 // A wave's running state: 32 columns of rows, two lanes a column.
 template <typename T, int DK, int DV>
 struct FwdWave {
@@ -97,10 +101,11 @@ struct FwdWave {
         // The reference follows the maximum only where a weight would pass 2^8: bfloat16
         // weights keep their relative precision at any reference; float16 ones are 2^6
         // times as large (T::kUp), so that small ones have their bits too.
-        if (__any((top - m) * c > 8.0f)) {
+        // (2^-120: a first key is always that far above kNoKey)
+        if (__any((top - m) * fmaxf(c, 0x1p-120f) > 8.0f)) {
             const float to = fmaxf(top, m);
-            // (no key seen yet: m and top are -inf, and the factor is that of a sum of nothing)
-            const float f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m - to) * c);
+            // (no key seen yet: the factor is that of a sum of nothing)
+            const float f = m == kNoKey ? 0.0f : __builtin_amdgcn_exp2f((m - to) * c);
             m = to;
             l *= f;
 #pragma unroll
@@ -108,7 +113,7 @@ struct FwdWave {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) o[t][r] *= f;
         }
-        const float mc = m == -INFINITY ? 0.0f : m * c - T::kUp;
+        const float mc = m == kNoKey ? 0.0f : m * c - T::kUp;
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
             float sum = 0.0f;
@@ -156,7 +161,7 @@ __global__ __launch_bounds__(256 * HALVES, ROWS == 128 ? 2 : 1) void full_fwd_ke
     load_columns<DK>(w.q, a.q + (j.q_lo + (int64_t)token) * a.q_row + head * a.q_head, lane);
 #pragma unroll
     for (int t = 0; t < kT; ++t) clear(w.o[t]);
-    w.m = -INFINITY;
+    w.m = kNoKey;
     w.l = 0.0f;
     w.lim = sees(row);
 
@@ -197,7 +202,7 @@ __global__ __launch_bounds__(256 * HALVES, ROWS == 128 ? 2 : 1) void full_fwd_ke
     }
 
     const float2 ls = both_halves(w.l);
-    float l = ls.x + ls.y, mc = w.m == -INFINITY ? -INFINITY : w.m * c - T::kUp;
+    float l = ls.x + ls.y, mc = w.m == kNoKey ? -INFINITY : w.m * c - T::kUp;
     const int h = lane >> 5;
     if constexpr (HALVES > 1) {
         // the second half's sums to LDS, a piece of 32 columns at a time [wave][piece][4 registers][lane], then added
