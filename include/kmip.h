@@ -370,8 +370,9 @@ kmip_status_t kmip_full_fwd(const void* Q, const void* K, const void* V, int32_t
  *        and keys that no query sees, get 0.
  *   p and g are rounded to the inputs' type for the products; every sum is in
  *   float32 and has one owner, so results are the same from call to call.
- *   float16: a g_ij beyond 65504 is an infinity, and p_ij and g_ij below 2^-14 are
- *   multiples of 2^-24 (scale dOut up, as in any training in float16).
+ *   float16: a g_ij beyond 65504 is an infinity, and those below 2^-14 are multiples of
+ *   2^-24 (scale dOut up, as in any training in float16); p_ij below 2^-23 are
+ *   multiples of 2^-33.
  *   workspace: kmip_full_bwd_workspace_size() bytes, 256-byte aligned.
  */
 size_t kmip_full_bwd_workspace_size(const int32_t* q_offsets, const int32_t* k_offsets, const int32_t* k_lengths,

@@ -17,7 +17,9 @@
 // p and g are rounded to the inputs' type for the products, half a step of each:
 // gradients are then off by 0.0025 of their size (bf16, against 64 bits) instead
 // of 0.0017, the rounding of the result itself.  A second product for what is
-// rounded off would cost a third of the matrix instructions more.
+// rounded off would cost a third of the matrix instructions more.  In float16 p is
+// 2^9 times as large (kUpBack) and dv divided by it at the end; g, whose size is
+// the caller's choice of dout's, is not.
 //
 // Measured (MI355X): 8192 tokens, 8 heads on 2 key heads, d = 128, causal: dq 200 us,
 // dk and dv 280, their runs' sums 14.  Bound as the forward is: matrix units
@@ -298,7 +300,10 @@ __global__ __launch_bounds__(256 * HALVES, KEYS == 128 ? 2 : 1) void full_dkv_ke
                 f32x4 di = {0.0f, 0.0f, 0.0f, 0.0f};
                 if constexpr (!kStart) di = *reinterpret_cast<const f32x4*>(sb + kTile + 2 * r);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) dp[r + e] = s[r + e] * (dp[r + e] + di[e]);
+                for (int e = 0; e < 4; ++e) {
+                    dp[r + e] = s[r + e] * (dp[r + e] + di[e]);
+                    s[r + e] *= T::kUpBack;   // (1 in bfloat16)
+                }
             }
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
@@ -358,7 +363,7 @@ __global__ __launch_bounds__(256 * HALVES, KEYS == 128 ? 2 : 1) void full_dkv_ke
             if (runs > 1)
                 store_sums<DV>(a.part_dv + (job * KEYS + (key - tile_lo)) * DV, dv[t], t, lane);
             else
-                store_piece<T, DV>(a.dv_out + at * DV, dv[t], t, 1.0f, lane);
+                store_piece<T, DV>(a.dv_out + at * DV, dv[t], t, 1.0f / T::kUpBack, lane);
         }
     } else {
         // tiles first + wave + 4 i
@@ -389,7 +394,7 @@ __global__ __launch_bounds__(256 * HALVES, KEYS == 128 ? 2 : 1) void full_dkv_ke
             }
         };
         join(dk, std::integral_constant<int, DK>(), a.part_dk, a.dk, a.scale);
-        join(dv, std::integral_constant<int, DV>(), a.part_dv, a.dv_out, 1.0f);
+        join(dv, std::integral_constant<int, DV>(), a.part_dv, a.dv_out, 1.0f / T::kUpBack);
     }
 }
 
@@ -488,7 +493,7 @@ hipError_t launch_bwd(const FullCall& f, const FullPlan& dq, const FullPlan& dkv
             hipLaunchKernelGGL((full_dkv_kernel<T, DK, DV, 128, 1>), dim3(l.jobs), dim3(256), 0, stream, a);
         hipError_t e = hipGetLastError();
         if (e == hipSuccess && l.tile_jobs > 0) {
-            SumArgs b{{ws.dk, ws.dv}, {a.dk, a.dv_out}, {f.d, f.dv}, {f.scale, 1.0f}};
+            SumArgs b{{ws.dk, ws.dv}, {a.dk, a.dv_out}, {f.d, f.dv}, {f.scale, 1.0f / T::kUpBack}};
             e = launch_sum<T>(b, a, l, dkv, true, stream);
         }
         if (e != hipSuccess) return e;

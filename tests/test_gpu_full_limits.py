@@ -41,3 +41,19 @@ def test_smallest_scales(m, n, scale, dtype):
     size = v.double().abs().cumsum(0)[sees[~none] - 1] / sees[~none][:, None, None]
     u = torch.finfo(dtype).eps / 2
     assert ((out[~none].double() - total).abs() <= u * total.abs() + n * 2.0 ** -23 * size + (2.0 ** -25 if dtype == HF else 0)).all()
+
+
+@pytest.mark.parametrize("m,n", [(1, 50_001), (40, 50_001), (1, 300_003), (2048, 30_011)])
+def test_many_alike_keys_backward_float16(m, n):
+    """Weights of 1 / n, among or below float16's subnormal numbers: their products with dout keep their bits."""
+    q, k = (torch.zeros(rows, 1, 16, dtype=HF, device="cuda") for rows in (m, n))
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    v, g = (torch.randn(rows, 1, 16, generator=gen, device="cuda").to(HF) for rows in (n, m))
+    g = (g.abs() + 1.0) * 64.0
+    out, lse = kmip.full_fwd(q, k, v, 0.25)
+    dv = kmip.full_bwd(q, k, v, g, out, lse, 0.25)[2]
+    want = g.double().sum(0) / n
+    # a weight off by half a step (2^-11), its exponent by lse's and its own roundings (2^-22 of 17.4 at most), m sums in 32 bits,
+    # the result's half step (2^-25 among subnormal numbers)
+    bound = want * (2.0 ** -11 + 2.0 ** -17 + m * 2.0 ** -24 + 2.0 ** -11) + 2.0 ** -25
+    assert ((dv.double() - want).abs() <= bound).all()
