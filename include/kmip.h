@@ -368,6 +368,10 @@ kmip_status_t kmip_full_fwd(const void* Q, const void* K, const void* V, int32_t
  *   out: dQ [Nq, H, d], dK [Nk, Hk, d], dV [Nk, Hk, dv] of the inputs' type,
  *        contiguous, overwritten whole: rows of a slot behind its keys in use,
  *        and keys that no query sees, get 0.
+ *   p is formed from lse, a float32: the weights of a row, and its gradients with
+ *   them, are off by a factor of up to exp(|lse_i| 2^-22), which is half a step of
+ *   float16 at |lse_i| = 2^11, of bfloat16 at 2^14 and 6% at 2^18.  Where K's rows are
+ *   nearly alike, dQ is what is left of terms that cancel, and the rounding of g shows in it.
  *   p and g are rounded to the inputs' type for the products; every sum is in
  *   float32 and has one owner, so results are the same from call to call.
  *   float16: a g_ij beyond 65504 is an infinity, and those below 2^-14 are multiples of

@@ -6,6 +6,8 @@ import pytest
 torch = pytest.importorskip("torch")
 kmip = pytest.importorskip("paper_2604_03815_amd")
 
+from full_reference import check, full64, sequences  # noqa: E402
+
 pytestmark = pytest.mark.gpu
 BF, HF, SF = torch.bfloat16, torch.float16, torch.float32
 
@@ -57,3 +59,43 @@ def test_many_alike_keys_backward_float16(m, n):
     # the result's half step (2^-25 among subnormal numbers)
     bound = want * (2.0 ** -11 + 2.0 ** -17 + m * 2.0 ** -24 + 2.0 ** -11) + 2.0 ** -25
     assert ((dv.double() - want).abs() <= bound).all()
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("size", [2.0 ** 8, 2.0 ** 12, 2.0 ** 16, 2.0 ** 20])
+@pytest.mark.parametrize("m,n", [(3, 90), (700, 700)])
+def test_gradients_of_large_scores(m, n, size, dtype):
+    """Scores of about `size`, of either sign, that differ by a few: weights come back from one float32 lse, off by |lse| 2^-22
+    in their exponent, which the reference's bound holds (2 (|scale s| 2^-22 and the product's own))."""
+    H, d = 2, 16
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    q, k, v, g = (torch.randn(rows, H, d, generator=gen, device="cuda") for rows in (m, n, n, m))
+    # one dimension makes the size, the others the differences
+    k = k * (0.5 if size <= 2.0 ** 12 else 8.0)
+    q[..., 0] = size ** 0.5
+    q[:, 1, 0] *= -1.0
+    k[..., 0] = size ** 0.5
+    q, k, v, g = (t.to(dtype) for t in (q, k, v, g))
+    out, lse = kmip.full_fwd(q, k, v, 1.0, causal=True)
+    dq, dk, dv = kmip.full_bwd(q, k, v, g, out, lse, 1.0, causal=True)
+    want = full64(q, k, v, 1.0, sequences(m, n), True, g)
+    # The reference's bound is relative, and scores 2^8 apart give weights below the smallest normal float32, 2^-126, for which 0
+    # may come out.  Up to 700 of them meet |dp - D| <= 2 * 16 * 5 * 5 < 2^10 and |q|, |k| <= 2^10: 2^9.5 * 2^20 * 2^-126 < 2^-96.
+    for name, x in dict(out=out, lse=lse, dq=dq, dk=dk, dv=dv).items():
+        value, bound = want[name]
+        check(name, x, (value, bound + 2.0 ** -96))
+
+
+@pytest.mark.parametrize("slope", [0.02, -0.02])
+def test_gradients_of_scores_far_apart(slope):
+    """Scores that rise and fall by hundreds from tile to tile: every gradient."""
+    n, d = 700, 64
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    q, k, v, g = (torch.randn(n, 2, d, generator=gen, device="cuda").to(HF) for _ in range(4))
+    steep = (k.float() * 0.1 + slope * torch.arange(n, device="cuda")[:, None, None] * torch.sign(q[:1].float())).to(HF)
+    same = q[:1].expand(n, 2, d).contiguous()
+    out, lse = kmip.full_fwd(same, steep, v, 1.0)
+    dq, dk, dv = kmip.full_bwd(same, steep, v, g, out, lse, 1.0)
+    want = full64(same, steep, v, 1.0, sequences(n, n), False, g)
+    for name, x in dict(out=out, lse=lse, dq=dq, dk=dk, dv=dv).items():
+        check(name, x, want[name])
