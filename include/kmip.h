@@ -377,6 +377,9 @@ kmip_status_t kmip_full_fwd(const void* Q, const void* K, const void* V, int32_t
  *   float16: a g_ij beyond 65504 is an infinity, and those below 2^-14 are multiples of
  *   2^-24 (scale dOut up, as in any training in float16); p_ij below 2^-23 are
  *   multiples of 2^-33.
+ *   A value of dOut that is not finite (a loss scaled too far) leaves dQ of its row, dK of
+ *   every key that the row sees and, in its column, their dV not finite; a g_ij that
+ *   overflows dQ_i and dK_j.  Other gradients of the same sequence may be not finite then, too.
  *   workspace: kmip_full_bwd_workspace_size() bytes, 256-byte aligned.
  */
 size_t kmip_full_bwd_workspace_size(const int32_t* q_offsets, const int32_t* k_offsets, const int32_t* k_lengths,

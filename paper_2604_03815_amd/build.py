@@ -16,13 +16,16 @@ FLAGS = [
     "-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950",
     # hand-written kernels must not get packed fp32 arithmetic from the compiler
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
-    # scores never hold NaN (finite bf16 inputs): lets max3 chains skip the
-    # IEEE quieting of each operand
-    "-Xarch_device", "-fno-honor-nans",
     # keep MFMA results in ordinary VGPRs, next to the VALU code that reads them
     "-mllvm", "-amdgpu-mfma-vgpr-form=1",
     "-Wall", "-Wno-unused-function",
 ]
+
+# scores never hold NaN (finite bf16 inputs): lets max3 chains skip the IEEE
+# quieting of each operand
+NO_NANS = ["-Xarch_device", "-fno-honor-nans"]
+# (gradients that are not finite are an answer: a loss was scaled too far)
+WITH_NANS = {"full_bwd.hip"}
 
 
 def sources():
@@ -38,7 +41,8 @@ def build(verbose: bool = False, jobs: int = 8) -> str:
 
     def compile_one(src):
         obj = os.path.join(objdir, os.path.basename(src) + tag)
-        cmd = [HIPCC, *FLAGS, *inc, "-c", src, "-o", obj]
+        nans = [] if os.path.basename(src) in WITH_NANS else NO_NANS
+        cmd = [HIPCC, *FLAGS, *nans, *inc, "-c", src, "-o", obj]
         if verbose:
             print(" ".join(cmd), flush=True)
         subprocess.check_call(cmd)

@@ -99,3 +99,40 @@ def test_gradients_of_scores_far_apart(slope):
     want = full64(same, steep, v, 1.0, sequences(n, n), False, g)
     for name, x in dict(out=out, lse=lse, dq=dq, dk=dk, dv=dv).items():
         check(name, x, want[name])
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("d,dv", [(16, 16), (64, 64), (128, 128)])
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+@pytest.mark.parametrize("m", [50, 4096])
+def test_gradients_that_are_not_finite(m, bad, d, dv, dtype):
+    """An infinity or a NaN in dout comes out in the gradients it enters, and in no other sequence's."""
+    H, offsets = 2, [0, m, m + 70]
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    q, k, v, g = (torch.randn(m + 70, H, w, generator=gen, device="cuda").to(dtype) for w in (d, d, dv, dv))
+    row, head, column = m // 2, 1, 5
+    clean = []
+    for value in (1.0, bad):
+        g[row, head, column] = value
+        out, lse = kmip.full_fwd(q, k, v, d ** -0.5, graph_offsets=offsets, causal=True)
+        clean.append(kmip.full_bwd(q, k, v, g, out, lse, d ** -0.5, graph_offsets=offsets, causal=True))
+    (dq0, dk0, dv0), (dq, dk, dvv) = clean
+    assert not torch.isfinite(dq[row, head]).any()
+    assert not torch.isfinite(dk[:row + 1, head]).any() and not torch.isfinite(dvv[:row + 1, head, column]).any()
+    for x, y in ((dq, dq0), (dk, dk0), (dvv, dv0)):
+        assert torch.equal(x[m:], y[m:]) and torch.equal(x[:m, 0], y[:m, 0])
+
+
+def test_overflow_of_float16_gradients():
+    """dout so large that p (dp - D) passes 65504: not finite, so that a scaled loss is seen to be scaled too far."""
+    q, k = (torch.zeros(n, 1, 16, dtype=HF, device="cuda") for n in (3, 2))
+    k[:] = 1.0   # (alike keys: both weights are 1/2)
+    v = torch.zeros(2, 1, 16, dtype=HF, device="cuda")
+    v[0], v[1] = 30.0, -30.0
+    g = torch.full((3, 1, 16), 1.0, dtype=HF, device="cuda")
+    g[1] = 1000.0   # dp = +-480,000, D = 0
+    out, lse = kmip.full_fwd(q, k, v, 1.0)
+    dq, dk, dv = kmip.full_bwd(q, k, v, g, out, lse, 1.0)
+    assert torch.isfinite(dq[[0, 2]]).all() and not torch.isfinite(dq[1]).any()
+    assert not torch.isfinite(dk).any()
+    assert torch.equal(dv, torch.full_like(dv, 501.0))
