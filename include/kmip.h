@@ -406,7 +406,9 @@ kmip_status_t kmip_full_bwd(const void* Q, const void* K, const void* V, const v
  *  - positions: device int32 [N], any values, or NULL: row i is at position i.
  *  - freqs: HOST float64 [rot / 2], read before the call returns (they travel in the
  *    kernel's arguments; the call can be captured into a HIP graph).
- *    The angle of position p is exact to |p| 2^-53 of the angle a position plus 2^-31 radians.
+ *    Sine and cosine are within 2^-22 of those of position * freqs[i], near and far: the
+ *    angle is reduced in fractions of a turn, off by 2^-28 radians (and 2^-62 of itself) at
+ *    most, and the two are float32.
  */
 kmip_status_t kmip_rotary(const void* X, void* Y, int32_t H, const void* X2, void* Y2, int32_t H2, int32_t dtype_in,
                           int32_t dtype_out, const int64_t* strides, const int32_t* positions, const double* freqs,

@@ -5,11 +5,14 @@
 // The gradient of a turn is the turn back, so one kernel serves both.
 //
 // Angles: the frequency in turns a position is held as a 64-bit fraction, so
-// position * frequency modulo one turn is one wrapping integer product, exact
-// but for the fraction's own rounding (position * 2^-63 turns): far positions
-// lose nothing.  Its top two bits (rounded) pick the quadrant; the rest, at most
+// position * frequency modulo one turn is one wrapping integer product: far
+// positions lose nothing.  The fraction is cut off at 2^-63 turns, times a position
+// of at most 2^31, and the product's top 32 bits are used: off by less than 2^-32
+// turns twice, 2^-28 radians.  Its top two bits (rounded) pick the quadrant; the rest, at most
 // pi/4, goes through the Taylor sums of sine and cosine (to x^9 and x^10:
-// remainders below 2e-9).  All in float32; the row's values are rounded once.
+// remainders below 2e-9).  All in float32 (the rest's conversion, its factor and
+// their product, 2.5 2^-24 of it, and the last sum's half step, 2^-25: below 2^-22 in
+// all); the row's values are rounded once.
 //
 // A thread takes P pairs of one token for up to four heads, so that an angle is
 // formed once for them; the threads of a token's heads are neighbours, so that
