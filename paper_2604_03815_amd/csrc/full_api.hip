@@ -132,14 +132,16 @@ kmip_status_t cut(std::vector<Seq>& seqs, bool causal, const Tiles& tiles_of, co
         l.jobs = (int32_t)jobs;
         l.tile_jobs = (int32_t)tile_jobs;
         l.first_job = (int32_t)p->jobs;
-        // two workgroups a CU are resident at once (see full_tile)
+        // two workgroups a CU are resident at once, or more (see full_tile)
         l.fold = p->halves == 1 && causal && jobs <= 512;
         p->jobs += jobs;
     }
     return KMIP_OK;
 }
 
-constexpr int64_t kSlots = 512;   // workgroups resident at once, two on each of 256 CUs
+// Workgroups that are resident at once whatever the widths, two on each of 256 CUs (at d, d_V <= 64 a CU holds up to four of the
+// one-group kernels: the plan has one number for all of them).
+constexpr int64_t kSlots = 512;
 
 int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
@@ -158,14 +160,20 @@ int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 // Two groups of waves on a 128-row tile (halves; only_halves: the kernel has no
 // other form): a CU works on one tile at a time and the last ones take half as
 // long, but the groups' sums have to be added and fewer workgroups share a CU.
-// So where there are few jobs and they are long; up to a whole round of CUs earlier than
-// with more, and at narrow widths, whose sums are small, too.  us with one group and with two:
+// So at narrow widths, whose sums are small, where there are few jobs and they are long.
+// us with one group and with two:
 //   d = 32, causal, forward and backward: 16 heads, 3000 tokens 119, 103; 4 texts of 2048, 8 heads 115, 105
 //   d = 64, the same: 8 heads, 4 texts of up to 2000 (208 jobs) 104, 77; 16 heads, 3000 tokens (376) 173, 159,
 //     4096 tokens (512) 238, 206; 8 heads, 8 texts of up to 2000 (800 jobs of 1500 rows) 156, 169;
 //     all pairs, 8 graphs of 1024 (512 jobs) 99, 108
-//   d = 128, 8 heads, causal, forward: 8192 tokens 182, 165; 4096 tokens 88, 71; 12 heads, 3000 tokens, all
-//     pairs 87, 104 (288 tiles: two rounds on 256 CUs)
+// At d = d_V = 128 one workgroup of two groups or two of one fill a CU.  Two groups win where causal jobs, of unequal
+// length, make one to two rounds of CUs, and where jobs make a whole round; with fewer, one group has runs, with more, jobs
+// that wait fill the gaps.  us of the forward with one group and with two (a head's tokens x heads: jobs):
+//   causal: 8192 x 3: 192 96, 98; 4096 x 8: 256 82, 64; 8192 x 5: 320 157, 123; 16,384 x 3: 384 306, 245;
+//     8192 x 8: 512 169, 145; 2048 x 32: 512 50, 49; 6144 x 12: 576 142, 138; 2304 x 32: 576 59, 64;
+//     8192 x 10: 640 194, 196; 8192 x 12: 768 207, 230; 16,384 x 8: 1024 542, 541; 8192 x 32: 2048 517, 556
+//   all pairs: 3900 x 8: 243 93, 120; 4096 x 8: 256 92, 78; 2048 x 16: 256 62, 45; 4200 x 8: 262 115, 135;
+//     6144 x 8: 384 173, 190; 8192 x 8: 512 260, 271; 8192 x 16: 1024 506, 535
 template <typename Kept, typename Streamed>
 kmip_status_t plan(std::vector<Seq>& seqs, int32_t Hk, bool causal, const Kept& kept_of, const Streamed& streamed_of,
                    int32_t width, bool only_halves, FullPlan* p) {
@@ -181,12 +189,9 @@ kmip_status_t plan(std::vector<Seq>& seqs, int32_t Hk, bool causal, const Kept& 
     const bool full = 2 * kept >= 128 * jobs;
     p->rows = full && (jobs >= kSlots || work >= kSlots * 512) ? 128 : 32;
     const int64_t half_slots = kSlots / 2;
-    // jobs >= half_slots run in whole rounds, or shorter ones fill the gaps
-    const bool rounds = jobs >= half_slots && (causal || 4 * jobs >= 3 * round_up(jobs, half_slots));
     const int64_t least = width <= 64 || jobs <= half_slots ? 1024 : 2048;
     const bool halves = width <= 192 ? jobs <= 2 * kSlots && work >= jobs * least
-                                     : (jobs <= 2 * kSlots && work >= jobs * 6144) ||
-                                           (rounds && jobs < kSlots && work >= jobs * 2048);
+                                     : (jobs == half_slots || (causal && jobs > half_slots && jobs <= kSlots)) && work >= jobs * 2048;
     p->halves = p->rows == 128 && (only_halves || halves) ? 2 : 1;
     int64_t run = 0;
     if (p->rows == 32)
