@@ -343,6 +343,9 @@ kmip_status_t kmip_fwd_noalloc(const void* Q, const void* K, const void* V, int6
  *    has KMIP_FULL_LONG keys, and often else.
  *  - Results do not depend on the other sequences' values and are the same from
  *    call to call (no atomics).
+ *  - A call's sequences are cut into jobs alike.  Single tokens over long caches and
+ *    long prompts are faster in calls of their own (4096 tokens, and one over 65,536
+ *    keys: 45 and 17 us, in one call 594).
  */
 #define KMIP_FULL_LONG 1024
 typedef enum { KMIP_BF16 = 0, KMIP_FP16 = 1, KMIP_FP32 = 2 } kmip_dtype_t;

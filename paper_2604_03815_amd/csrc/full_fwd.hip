@@ -25,9 +25,9 @@
 //
 // Measured (MI355X) and what bounds it:
 //   - d = 128: matrix and vector instructions, which overlap in part, and power
-//     (2.0 to 2.2 GHz).  A prompt of 16,384 tokens, 8 heads on 2 key heads, causal: 545
-//     us, 1.01 PFLOP/s (a library product of 8192^3: 1.2); the matrix units are busy 48% of the
-//     time, the vector units issue 40% of it.  Interleaving the scores of a
+//     (2.0 to 2.2 GHz).  A prompt of 16,384 tokens, 8 heads on 2 key heads, causal: 540
+//     us, 1.02 PFLOP/s (a library product of 8192^3: 1.2); the matrix units are busy 58% of the
+//     time, the vector units issue 48% of it.  Interleaving the scores of a
 //     tile, the weights of the one before and the product of the one before that
 //     in one block of code gave nothing (580 us for 584 then).
 //   - d <= 64: vector issue.  64 keys of 32 rows at d = 64 are 98 vector

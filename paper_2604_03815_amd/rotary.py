@@ -77,6 +77,7 @@ def rotary(q, k_=None, positions=None, freqs=None, interleaved: bool = False, ma
     (default: the inputs'): bfloat16, float16 or float32.  inverse turns back.  q_out, k_out: tensors to write into,
     q_out=q for in place.  Inputs and outputs may be views whose last dimension is contiguous (outputs must not overlap themselves).
     Differentiable in q and k_ unless q_out or k_out is given; once, and in reverse mode only (dual tensors are refused).
+    For a backward in a HIP graph see ``full_attention``.
     """
     if freqs is None:
         raise ValueError("freqs must be given (see rotary_frequencies)")
