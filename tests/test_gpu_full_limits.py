@@ -136,3 +136,41 @@ def test_overflow_of_float16_gradients():
     assert torch.isfinite(dq[[0, 2]]).all() and not torch.isfinite(dq[1]).any()
     assert not torch.isfinite(dk).any()
     assert torch.equal(dv, torch.full_like(dv, 501.0))
+
+
+def test_queries_past_32_bits():
+    """Queries, gradients and results behind the first 4 GB of their tensors; the rows before them see no key."""
+    far, m, n, H, d = (1 << 23) + 1000, 77, 130, 2, 128
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    k, v = (torch.randn(n, 1, d, generator=gen, device="cuda").to(BF) for _ in range(2))
+    q, g = (torch.zeros(far + m, H, d, dtype=BF, device="cuda") for _ in range(2))
+    q[far:], g[far:] = (torch.randn(m, H, d, generator=gen, device="cuda").to(BF) for _ in range(2))
+    where = dict(graph_offsets=[0, far, far + m], key_offsets=[0, 0, n])
+    out, lse = kmip.full_fwd(q, k, v, 0.1, causal=True, **where)
+    dq, dk, dv = kmip.full_bwd(q, k, v, g, out, lse, 0.1, causal=True, **where)
+    assert not out[:far].any() and (lse[:far] == -math.inf).all() and not dq[:far].any()
+    want = full64(q[far:], k, v, 0.1, sequences(m, n), True, g[far:])
+    for name, x in dict(out=out[far:], lse=lse[far:], dq=dq[far:], dk=dk, dv=dv).items():
+        check(name, x, want[name])
+
+
+@pytest.mark.parametrize("d,dv", [(16, 16), (128, 128), (32, 64)])
+@pytest.mark.parametrize("m", [150, 20])
+def test_rows_far_apart(m, d, dv):
+    """Rows as far apart as a call takes them (2^23 - 8 values): views give what their copies give."""
+    n, stride = 150, 2 ** 23 - 8
+    H, Hk = (256, 256) if m == 150 else (4, 2)   # (tiles of 128 rows, of 32)
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    whole = torch.zeros(n * stride, dtype=BF, device="cuda")
+    at, views = 0, []
+    for rows, heads, width in ((m, H, d), (n, Hk, d), (n, Hk, dv), (m, H, dv)):
+        view = torch.as_strided(whole, (rows, heads, width), (stride, width, 1), at)
+        view.copy_(torch.randn(rows, heads, width, generator=gen, device="cuda").to(BF))
+        views.append(view)
+        at += heads * width
+    results = []
+    for q, k, v, g in (views, [t.contiguous() for t in views]):
+        out, lse = kmip.full_fwd(q, k, v, 0.1)
+        results.append((out, lse, *kmip.full_bwd(q, k, v, g, out, lse, 0.1)))
+    for x, y in zip(*results):
+        assert torch.equal(x, y)

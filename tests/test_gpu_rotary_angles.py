@@ -54,3 +54,16 @@ def test_sine_and_cosine(seed, fast):
     far = np.abs(np.outer(positions, freqs)) * 2.0 ** -62
     bound = 2.0 ** -22 + 2.0 ** -28 + far
     assert (np.abs(got[:, :64] - np.cos(angle)) <= bound).all() and (np.abs(got[:, 64:] - np.sin(angle)) <= bound).all()
+
+
+@pytest.mark.parametrize("rot", [128, 126])   # (runs of 16 bytes, and pair by pair)
+def test_rows_past_32_bits(rot):
+    """Rows behind the first 4 GB, turned in place, are what the same rows give by themselves; the others are zeros and stay zeros."""
+    n, last, d = (1 << 24) + 3000, 300, 128
+    freqs, _ = kmip.rotary_frequencies(rot)
+    rows = torch.randn(last, 1, d, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda").to(torch.bfloat16)
+    x = torch.zeros(n, 1, d, dtype=torch.bfloat16, device="cuda")
+    x[-last:] = rows
+    kmip.rotary(x, freqs=freqs, q_out=x)
+    positions = torch.arange(n - last, n, dtype=torch.int32, device="cuda")
+    assert torch.equal(x[-last:], kmip.rotary(rows, None, positions, freqs)) and not x[:-last].any()
