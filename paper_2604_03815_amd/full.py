@@ -15,7 +15,7 @@ with room.  Without graph_offsets there is one sequence.  ``causal``: the querie
 last positions of their sequence, query t of m sees keys 0 .. t + n - m of n.
 The offsets and lengths are read when the call is made: a captured call keeps them.
 Inputs are finite (rows behind the keys in use may hold anything: they are not read);
-given outputs overlap neither inputs nor each other.  A call's sequences are cut into jobs alike: single tokens over long
+given outputs overlap neither inputs nor each other, and require no gradient (unless under torch.no_grad()).  A call's sequences are cut into jobs alike: single tokens over long
 caches and long prompts are faster in calls of their own.
 """
 from __future__ import annotations
